@@ -21,6 +21,9 @@
  *   orloj_sched_*           host runtime: per-model deadline queues, drop
  *                           phase, one score + select round per call
  *   orloj_simulate_trace    trace-driven worker simulation on that runtime
+ *   orloj_worker_*          the worker's side of a batch: adapters of its
+ *                           members' applications, a quantised paged cache
+ *                           of keys and values, attention over it
  *
  * Conventions.  Pointers named d_* are device (HBM) pointers owned by the
  * caller; h_* pointers and the structs are host memory read during the call
@@ -490,6 +493,165 @@ int orloj_simulate_trace(orloj_sched *s, const orloj_trace *trace, double tick_m
                          const uint32_t *h_solo_counts, const double *h_bin_width_ms,
                          const double *h_bs_scale, uint64_t seed, int64_t max_ticks,
                          orloj_sim_record *rec, orloj_sim_stats *out);
+
+/*
+ * The worker's side of a batch (§3.1: a worker runs one batch of a model at a
+ * time; §3.2 "Per-Application Tracking": the members of a batch belong to
+ * different applications of the model).  The operators of a text model's step
+ * that depend on what the scheduler put together: rows of different
+ * applications, requests of different lengths.
+ *
+ * A worker handle holds scratch memory and a device status word.  Calls
+ * enqueue on its context's stream, as every call of the library does;
+ * failures found on the host are described by orloj_last_error of the
+ * context.  Problems found in device data (named at each call) are recorded
+ * and returned by orloj_worker_sync as ORLOJ_E_DATA; the outputs of the rows
+ * concerned are then unspecified, nothing is read or written out of bounds.
+ * Scratch grows on demand (ORLOJ_E_NOMEM if that fails); grown blocks are kept
+ * until orloj_worker_destroy, so captured calls keep theirs.  A stream under
+ * capture cannot grow it: make a call of the same sizes before the capture
+ * (else ORLOJ_E_INVALID).  A worker is not thread-safe, and calls or replays
+ * that may overlap on the device need a worker each.  When the context's
+ * stream has changed, the next call waits for the work enqueued on the
+ * previous one, which must still exist.
+ */
+typedef struct orloj_worker orloj_worker;
+
+int orloj_worker_create(orloj_worker **out, orloj_ctx *ctx);
+/* Waits for the worker's stream first, which must still exist.  NULL is a no-op.
+ * The context may have been destroyed before. */
+void orloj_worker_destroy(orloj_worker *worker);
+/* Wait for the work enqueued on the context's stream, then report and clear
+ * any data error the worker's calls found (ORLOJ_E_DATA). */
+int orloj_worker_sync(orloj_worker *worker);
+
+/* Element types of activations and adapter weights. */
+enum orloj_dtype { ORLOJ_F32 = 0, ORLOJ_F16 = 1, ORLOJ_BF16 = 2 };
+
+/* Compiled limits. */
+#define ORLOJ_MAX_RANK 128     /* rank of an adapter */
+#define ORLOJ_MAX_HEAD_DIM 256 /* dimension of a cached key or value */
+#define ORLOJ_MAX_TREE 64      /* drafted tokens of a request */
+
+/*
+ * Low-rank adapters of a model's applications beside a projection they share.
+ * Row t of a batch belongs to adapter a = d_adapter[t], or to none (-1):
+ *   h_t = A_a x_t                    (A_a: the first rank_a rows of d_down[a])
+ *   y_t = base_t + s_a B_a h_t       (B_a: the first rank_a columns of d_up[a])
+ *   y_t = base_t                     without an adapter or at rank 0
+ * base_t is the shared projection's output; d_base = NULL takes zeros, and
+ * d_base may be d_y (with the same stride), no other overlap.  h, the sums and
+ * the addition are held in 32 bits or more; y is rounded once.  Rows of one
+ * adapter need not be adjacent, though weights are read once per 16
+ * adjacent rows that share them.
+ *
+ * dtype (ORLOJ_F16 or ORLOJ_BF16) is the type of d_x, d_base, d_y and the
+ * weights.  Strides are in elements between rows, at least d_in (x) or d_out
+ * (base, y).  Data errors: an adapter id outside [-1, n_adapters), a rank
+ * outside [0, rank].
+ */
+typedef struct orloj_adapters {
+    int32_t n_adapters;       /* >= 0 */
+    int32_t rank;             /* largest rank, [1, ORLOJ_MAX_RANK]: the layout's */
+    int32_t d_in, d_out;      /* >= 1 */
+    int32_t dtype;
+    const void *d_down;       /* device [n_adapters][rank][d_in] */
+    const void *d_up;         /* device [n_adapters][d_out][rank] */
+    const float *d_scale;     /* device [n_adapters]; NULL = 1 */
+    const int32_t *d_rank;    /* device [n_adapters]; NULL = rank */
+} orloj_adapters;
+
+int orloj_worker_adapt(orloj_worker *worker, const orloj_adapters *adapters, int64_t n_rows,
+                       const int32_t *d_adapter, const void *d_x, int64_t x_stride,
+                       const void *d_base, int64_t base_stride, void *d_y, int64_t y_stride);
+
+/*
+ * A paged cache of keys and values in 8 bits.  A page holds page_size tokens
+ * of every head; a request's tokens are on the pages its table lists, in
+ * order.  The vector of one (token, head) is stored as codes on one scale:
+ *   amax  = max_i |x_i|,  scale = amax (1 / top)
+ *   code_i = x_i ((1 / amax) top) rounded to nearest even: an integer (INT8, top =
+ *            127) or an e4m3 number (FP8, top = 448, no infinities)
+ * in 32-bit arithmetic; it stands for code_i * scale.  A vector with amax <
+ * 2^-100 is stored as zeros (codes and scale 0), one with an infinity or a NaN
+ * as NaN (codes 0, scale NaN).  Rows are padded to dim_pad = head_dim rounded
+ * up to a multiple of 64; the padding is written as zeros.
+ */
+enum orloj_cache_format { ORLOJ_CACHE_INT8 = 0, ORLOJ_CACHE_FP8 = 1 };
+
+typedef struct orloj_cache {
+    int32_t n_pages;          /* >= 0 */
+    int32_t page_size;        /* tokens: 16, 32, 64, 128 or 256 */
+    int32_t n_heads;          /* key / value heads, >= 1 */
+    int32_t head_dim;         /* [1, ORLOJ_MAX_HEAD_DIM] */
+    int32_t format;
+    void *d_k, *d_v;          /* device [n_pages][n_heads][page_size][dim_pad], 16-byte aligned */
+    float *d_k_scale, *d_v_scale; /* device [n_pages][n_heads][page_size] */
+} orloj_cache;
+
+/*
+ * The requests of a batch, their new tokens' rows stored back to back.  Request
+ * r has d_length[r] tokens, its rows d_row_off[r] .. d_row_off[r+1]-1 being the
+ * last of them.  Everything is device memory, so that a captured step can be
+ * replayed with other lengths; max_rows and max_length bound them on the host
+ * (they size launches).  Data errors: offsets that decrease or leave
+ * [0, n_rows], more rows than max_rows or than the length, a length beyond max_length
+ * or beyond the table, a needed page outside [0, n_pages).  Entries of the
+ * table past a request's last page are not read.
+ */
+typedef struct orloj_batch {
+    int32_t n_requests;       /* >= 0 */
+    int32_t max_pages;        /* entries of a request in the table, >= 0 */
+    int64_t n_rows;           /* d_row_off[n_requests], >= 0 */
+    int32_t max_rows;         /* of one request */
+    int32_t max_length;       /* of one request */
+    const int32_t *d_row_off; /* device [n_requests + 1] */
+    const int32_t *d_length;  /* device [n_requests] */
+    const int32_t *d_pages;   /* device [n_requests][max_pages] */
+} orloj_batch;
+
+/* [n_rows][heads][head_dim] activations: elements of a vector adjacent, strides
+ * in elements between rows and between heads (non-negative). */
+typedef struct orloj_vectors {
+    void *d;
+    int64_t row_stride, head_stride;
+} orloj_vectors;
+
+/* Write the rows' keys and values (dtype, any of the three) to their places in
+ * the cache.  Two rows at one place (a page shared by two requests): one of the
+ * two is kept. */
+int orloj_worker_cache_write(orloj_worker *worker, const orloj_cache *cache,
+                             const orloj_batch *batch, int32_t dtype, const orloj_vectors *k,
+                             const orloj_vectors *v);
+
+/* Read the rows' places back: code * scale in 32 bits, rounded once to dtype.
+ * With d_row_off the running sums of d_length, that is the whole cache. */
+int orloj_worker_cache_read(orloj_worker *worker, const orloj_cache *cache,
+                            const orloj_batch *batch, int32_t dtype, const orloj_vectors *k,
+                            const orloj_vectors *v);
+
+/*
+ * Attention of the rows over their requests' cached tokens (their own rows
+ * among them: write those first).  With n_q_heads = g n_heads query heads,
+ * head i reading key / value head i / g, for every row and head:
+ *   s_j = scale q . k_j,   p = softmax of s over the visible tokens j,
+ *   out = sum_j p_j v_j,   d_lse[row][i] = ln sum_j exp s_j   (NULL: not written)
+ * Token j < length - rows of the request is visible to every row.  Of the
+ * request's own rows, row i sees row j iff j <= i (d_tree = NULL: single
+ * tokens, chunks of a prompt), or iff bit j of d_tree[row] is set (a tree of
+ * drafted tokens: each names its ancestors and itself; max_rows <=
+ * ORLOJ_MAX_TREE; bits past the request's rows are ignored).  A row that sees nothing gets zeros and
+ * -infinity.  Tokens a row does not see have no effect on it, whatever they
+ * hold; one it sees with a NaN key or value makes it NaN.
+ * dtype (ORLOJ_F16 or ORLOJ_BF16) is the type of q and out.  The scores' sums,
+ * the softmax's statistics and the output's sums are held in 32 bits; q, scaled
+ * per row, and the weights enter the products in 16-bit floating point with 11
+ * significant bits, the codes exactly.  Results are the same bits every time
+ * for the same arguments.
+ */
+int orloj_worker_attend(orloj_worker *worker, const orloj_cache *cache, const orloj_batch *batch,
+                        int32_t dtype, int32_t n_q_heads, float scale, const orloj_vectors *q,
+                        const uint64_t *d_tree, const orloj_vectors *out, float *d_lse);
 
 #ifdef __cplusplus
 }

@@ -8,7 +8,7 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRCS = [os.path.join(HERE, "csrc", "orloj.hip"), os.path.join(HERE, "csrc", "sched.hip")]
+SRCS = [os.path.join(HERE, "csrc", f) for f in ("orloj.hip", "sched.hip", "worker.hip")]
 LIB = os.path.join(HERE, "liborloj.so")
 ARCH = os.environ.get("ORLOJ_OFFLOAD_ARCH", "gfx950")
 

@@ -56,6 +56,28 @@ class Trace(ctypes.Structure):
                 ("h_deadline_ms", ctypes.c_void_p)]
 
 
+class AdapterSet(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("n_adapters", "rank", "d_in", "d_out", "dtype")] + \
+               [(k, ctypes.c_void_p) for k in ("d_down", "d_up", "d_scale", "d_rank")]
+
+
+class PagedCache(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("n_pages", "page_size", "n_heads", "head_dim", "format")] + \
+               [(k, ctypes.c_void_p) for k in ("d_k", "d_v", "d_k_scale", "d_v_scale")]
+
+
+class BatchRows(ctypes.Structure):
+    _fields_ = [("n_requests", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("n_rows", ctypes.c_int64), ("max_rows", ctypes.c_int32),
+                ("max_length", ctypes.c_int32), ("d_row_off", ctypes.c_void_p),
+                ("d_length", ctypes.c_void_p), ("d_pages", ctypes.c_void_p)]
+
+
+class Vectors(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_void_p), ("row_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
 class SimStats(ctypes.Structure):
     _fields_ = [(k, ctypes.c_int64) for k in ("ticks", "launches", "decisions", "dispatched",
                                              "dropped", "on_time", "late", "arrivals")] + \
@@ -76,6 +98,10 @@ _GP = ctypes.POINTER(Grid)
 _QP = ctypes.POINTER(Queues)
 _SP = ctypes.POINTER(Steps)
 _I64P = ctypes.POINTER(ctypes.c_int64)
+_AP = ctypes.POINTER(AdapterSet)
+_CP = ctypes.POINTER(PagedCache)
+_BP = ctypes.POINTER(BatchRows)
+_VECP = ctypes.POINTER(Vectors)
 
 EXPORTS = ("orloj_create", "orloj_destroy", "orloj_set_stream", "orloj_set_score_chunk",
            "orloj_last_error", "orloj_sync",
@@ -84,7 +110,9 @@ EXPORTS = ("orloj_create", "orloj_destroy", "orloj_set_stream", "orloj_set_score
            "orloj_select_batch", "orloj_build_model_laws",
            "orloj_iterate", "orloj_accumulate", "orloj_sched_create", "orloj_sched_destroy",
            "orloj_sched_admit", "orloj_sched_decide", "orloj_sched_queue_length",
-           "orloj_simulate_trace")
+           "orloj_simulate_trace", "orloj_worker_create", "orloj_worker_destroy",
+           "orloj_worker_sync", "orloj_worker_adapt", "orloj_worker_cache_write",
+           "orloj_worker_cache_read", "orloj_worker_attend")
 
 
 def load(path: Optional[str] = None):
@@ -145,6 +173,22 @@ def load(path: Optional[str] = None):
                                        ctypes.c_uint64, ctypes.c_int64, ctypes.POINTER(SimRecord),
                                        ctypes.POINTER(SimStats)]
     L.orloj_simulate_trace.restype = ctypes.c_int
+    L.orloj_worker_create.argtypes = [ctypes.POINTER(_VP), _VP]
+    L.orloj_worker_create.restype = ctypes.c_int
+    L.orloj_worker_destroy.argtypes = [_VP]
+    L.orloj_worker_destroy.restype = None
+    L.orloj_worker_sync.argtypes = [_VP]
+    L.orloj_worker_sync.restype = ctypes.c_int
+    L.orloj_worker_adapt.argtypes = [_VP, _AP, ctypes.c_int64, _VP, _VP, ctypes.c_int64, _VP,
+                                     ctypes.c_int64, _VP, ctypes.c_int64]
+    L.orloj_worker_adapt.restype = ctypes.c_int
+    L.orloj_worker_cache_write.argtypes = [_VP, _CP, _BP, ctypes.c_int32, _VECP, _VECP]
+    L.orloj_worker_cache_write.restype = ctypes.c_int
+    L.orloj_worker_cache_read.argtypes = L.orloj_worker_cache_write.argtypes
+    L.orloj_worker_cache_read.restype = ctypes.c_int
+    L.orloj_worker_attend.argtypes = [_VP, _CP, _BP, ctypes.c_int32, ctypes.c_int32,
+                                      ctypes.c_float, _VECP, _VP, _VECP, _VP]
+    L.orloj_worker_attend.restype = ctypes.c_int
     if default:
         _LIB = L
     return L

@@ -1,0 +1,269 @@
+"""The worker's side of a batch: Python binding of orloj_worker_* (include/orloj.h).
+
+The scheduler hands out batches whose members belong to different applications of
+one model and have different lengths.  These are the operators of a text model's
+step that depend on that:
+
+  Adapters   low-rank adapters of the applications beside a projection they share
+  Cache      keys and values of the requests in 8 bits on pages: written, read
+             back, and attended to
+  Batch      the requests of a batch and their new tokens' rows
+
+Argument marshalling only, as in orloj.py: the work is done in the HIP kernels of
+liborloj.so, there is no fallback.  Calls enqueue on the stream of the worker's
+context and return tensors that are ready in that stream's order.
+"""
+from __future__ import annotations
+
+import ctypes
+import sys
+from typing import Optional, Tuple
+
+import torch
+
+from . import orloj as O
+
+DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+INT8, FP8 = 0, 1
+FORMATS = {torch.int8: INT8, torch.float8_e4m3fn: FP8}
+MAX_RANK, MAX_HEAD_DIM, MAX_TREE = 128, 256, 64
+
+
+def dim_pad(head_dim: int) -> int:
+    """Bytes a cached vector takes: head_dim rounded up to a multiple of 64."""
+    return (head_dim + 63) & ~63
+
+
+class Worker:
+    """An orloj_worker: the scratch memory and status word the operators of one
+    worker share.  Bound to a Context (its device and stream)."""
+
+    def __init__(self, ctx: Optional[O.Context] = None):
+        self.ctx = ctx or O.Context()
+        self.L = self.ctx.L
+        self.device = self.ctx.device
+        self.w = ctypes.c_void_p()
+        self.ctx._check(self.L.orloj_worker_create(ctypes.byref(self.w), self.ctx.ctx))
+
+    def __del__(self):
+        finalizing = sys is None or sys.is_finalizing()
+        if getattr(self, "w", None) and self.w.value and not finalizing:
+            self.L.orloj_worker_destroy(self.w)
+            self.w = None
+
+    def sync(self):
+        """Wait for the enqueued work; raises OrlojError (E_DATA) for what the
+        calls found wrong in device data."""
+        self.ctx._check(self.L.orloj_worker_sync(self.w))
+
+
+def _need(t, name, dtype, device):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must live on {device}, not {t.device}")
+
+
+def _rows(t, name, dtype, device, width):
+    """Row stride of a [rows, width] matrix whose rows are contiguous."""
+    _need(t, name, dtype, device)
+    if t.dim() != 2 or t.shape[1] != width:
+        raise ValueError(f"{name} must be [rows, {width}], not {list(t.shape)}")
+    if width > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else width
+
+
+def _vectors(t, name, dtype, device, rows, heads, dim):
+    """A [rows, heads, dim] tensor with contiguous vectors."""
+    _need(t, name, dtype, device)
+    if t.shape != (rows, heads, dim):
+        raise ValueError(f"{name} must be {[rows, heads, dim]}, not {list(t.shape)}")
+    if dim > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name} must have contiguous vectors")
+    return O.Vectors(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+class Adapters:
+    """Low-rank adapters of a model's applications: down [n, rank, d_in], up
+    [n, d_out, rank] (float16 or bfloat16), optional scale [n] (float32) and
+    rank [n] (int32: how much of the layout's rank each adapter uses)."""
+
+    def __init__(self, worker: Worker, down: torch.Tensor, up: torch.Tensor,
+                 scale: Optional[torch.Tensor] = None, rank: Optional[torch.Tensor] = None):
+        if down.dim() != 3 or up.dim() != 3 or down.shape[0] != up.shape[0] or down.shape[1] != up.shape[2]:
+            raise ValueError(f"down [n, rank, d_in] and up [n, d_out, rank] do not agree: "
+                             f"{list(down.shape)}, {list(up.shape)}")
+        O._need_cuda(down, "down", (torch.float16, torch.bfloat16), worker.device)
+        O._need_cuda(up, "up", (down.dtype,), worker.device)
+        n = down.shape[0]
+        for t, name, dt in ((scale, "scale", torch.float32), (rank, "rank", torch.int32)):
+            if t is not None:
+                O._need_cuda(t, name, (dt,), worker.device)
+                if t.shape != (n,):
+                    raise ValueError(f"{name} must be [{n}]")
+        self.worker = worker
+        self.dtype = down.dtype
+        self.d_in, self.d_out = down.shape[2], up.shape[1]
+        self._keep = (down, up, scale, rank)
+        self._set = O.AdapterSet(n, down.shape[1], self.d_in, self.d_out, DTYPES[down.dtype],
+                                 *(None if t is None else t.data_ptr() for t in self._keep))
+        self._ref = ctypes.byref(self._set)
+
+    def apply(self, x: torch.Tensor, adapter: torch.Tensor, base: Optional[torch.Tensor] = None,
+              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """base + scale * up[a] (down[a] x) per row, a = adapter[row] (int32; -1: base
+        alone).  x [rows, d_in]; base (the shared projection's output; None: zeros) and out
+        [rows, d_out]; out may be base."""
+        w = self.worker
+        xs = _rows(x, "x", self.dtype, w.device, self.d_in)
+        n = x.shape[0]
+        _need(adapter, "adapter", torch.int32, w.device)
+        if adapter.shape != (n,) or not adapter.is_contiguous():
+            raise ValueError(f"adapter must be a contiguous [{n}]")
+        if out is None:
+            out = torch.empty((n, self.d_out), dtype=self.dtype, device=w.device)
+        ys = _rows(out, "out", self.dtype, w.device, self.d_out)
+        bs, bp = 0, None
+        if base is not None:
+            bs, bp = _rows(base, "base", self.dtype, w.device, self.d_out), base.data_ptr()
+            if base.shape[0] != n:
+                raise ValueError("base and x differ in rows")
+        if out.shape[0] != n:
+            raise ValueError("out and x differ in rows")
+        rc = w.L.orloj_worker_adapt(w.w, self._ref, n, adapter.data_ptr(), x.data_ptr(), xs, bp, bs,
+                                    out.data_ptr(), ys)
+        if rc:
+            w.ctx._check(rc)
+        return out
+
+
+class Batch:
+    """The requests of a batch (device int32 tensors): row_off [n + 1] (their new
+    tokens' rows), length [n] (tokens of each, the rows the last of them), pages
+    [n, max_pages].  n_rows = row_off[n]; max_rows and max_length bound a request's
+    rows and length.  The bounds are read from the device where they are not given
+    (which waits for it)."""
+
+    def __init__(self, row_off: torch.Tensor, length: torch.Tensor, pages: torch.Tensor,
+                 n_rows: Optional[int] = None, max_rows: Optional[int] = None,
+                 max_length: Optional[int] = None):
+        n = length.shape[0] if length.dim() == 1 else -1
+        for t, name in ((row_off, "row_off"), (length, "length"), (pages, "pages")):
+            O._need_cuda(t, name, (torch.int32,), length.device)
+        if row_off.shape != (n + 1,) or pages.dim() != 2 or pages.shape[0] != n:
+            raise ValueError("row_off must be [n + 1], length [n] and pages [n, max_pages]")
+        if n_rows is None:
+            n_rows = int(row_off[-1])
+        if max_rows is None:
+            max_rows = int((row_off[1:] - row_off[:-1]).max()) if n else 0
+        if max_length is None:
+            max_length = int(length.max()) if n else 0
+        self.device = length.device
+        self.n_rows, self.max_rows, self.max_length = n_rows, max_rows, max_length
+        self._keep = (row_off, length, pages)
+        self._rows = O.BatchRows(n, pages.shape[1], n_rows, max_rows, max_length, row_off.data_ptr(),
+                                 length.data_ptr(), pages.data_ptr())
+        self._ref = ctypes.byref(self._rows)
+
+
+class Cache:
+    """A paged cache in 8 bits: k and v [n_pages, heads, page_size, dim_pad(head_dim)]
+    (int8 or float8_e4m3fn codes), k_scale and v_scale [n_pages, heads, page_size]
+    (float32)."""
+
+    def __init__(self, worker: Worker, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor,
+                 v_scale: torch.Tensor, head_dim: int):
+        O._need_cuda(k, "k", tuple(FORMATS), worker.device)
+        O._need_cuda(v, "v", (k.dtype,), worker.device)
+        O._need_cuda(k_scale, "k_scale", (torch.float32,), worker.device)
+        O._need_cuda(v_scale, "v_scale", (torch.float32,), worker.device)
+        if k.dim() != 4 or v.shape != k.shape or k.shape[3] != dim_pad(head_dim):
+            raise ValueError(f"k and v must be [n_pages, heads, page_size, {dim_pad(head_dim)}]")
+        if k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3]:
+            raise ValueError("k_scale and v_scale must be [n_pages, heads, page_size]")
+        self.worker = worker
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.heads, self.head_dim = k.shape[1], head_dim
+        self._cache = O.PagedCache(k.shape[0], k.shape[2], k.shape[1], head_dim, FORMATS[k.dtype], k.data_ptr(),
+                                   v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self._ref = ctypes.byref(self._cache)
+
+    @classmethod
+    def empty(cls, worker: Worker, n_pages: int, heads: int, head_dim: int, page_size: int = 16,
+              dtype: torch.dtype = torch.int8) -> "Cache":
+        """A cache with memory of its own."""
+        if dtype not in FORMATS:
+            raise TypeError(f"dtype {dtype} is not one of {tuple(FORMATS)}")
+        at = dict(device=worker.device)
+        k, v = (torch.empty(n_pages, heads, page_size, dim_pad(head_dim), dtype=dtype, **at) for _ in range(2))
+        ks, vs = (torch.empty(n_pages, heads, page_size, **at) for _ in range(2))
+        return cls(worker, k, v, ks, vs, head_dim)
+
+    def _check_batch(self, batch: Batch):
+        if batch.device != self.worker.device:
+            raise ValueError(f"the batch must live on {self.worker.device}, not {batch.device}")
+
+    def write(self, batch: Batch, k: torch.Tensor, v: torch.Tensor):
+        """Quantise the rows' keys and values [n_rows, heads, head_dim] (float32,
+        float16 or bfloat16) to their places."""
+        w = self.worker
+        self._check_batch(batch)
+        if k.dtype not in DTYPES:
+            raise TypeError(f"k has dtype {k.dtype}, expected one of {tuple(DTYPES)}")
+        kv = _vectors(k, "k", k.dtype, w.device, batch.n_rows, self.heads, self.head_dim)
+        vv = _vectors(v, "v", k.dtype, w.device, batch.n_rows, self.heads, self.head_dim)
+        rc = w.L.orloj_worker_cache_write(w.w, self._ref, batch._ref, DTYPES[k.dtype], kv, vv)
+        if rc:
+            w.ctx._check(rc)
+
+    def read(self, batch: Batch, dtype: torch.dtype = torch.bfloat16
+             ) -> Tuple[torch.Tensor, torch.Tensor]:
+        """The rows' keys and values as the cache holds them, [n_rows, heads, head_dim]."""
+        w = self.worker
+        self._check_batch(batch)
+        if dtype not in DTYPES:
+            raise TypeError(f"dtype {dtype} is not one of {tuple(DTYPES)}")
+        shape = (batch.n_rows, self.heads, self.head_dim)
+        k, v = torch.empty(shape, dtype=dtype, device=w.device), torch.empty(shape, dtype=dtype, device=w.device)
+        rc = w.L.orloj_worker_cache_read(w.w, self._ref, batch._ref, DTYPES[dtype],
+                                         _vectors(k, "k", dtype, w.device, *shape),
+                                         _vectors(v, "v", dtype, w.device, *shape))
+        if rc:
+            w.ctx._check(rc)
+        return k, v
+
+    def attend(self, batch: Batch, q: torch.Tensor, scale: Optional[float] = None,
+               tree: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+               lse: bool = False):
+        """Attention of the rows' queries q [n_rows, g * heads, head_dim] (float16 or
+        bfloat16) over their requests' tokens; scale defaults to 1 / sqrt(head_dim).
+        tree (int64 [n_rows]): bit j of a row's mask lets it see its request's row j
+        (None: the rows up to itself).  Returns out, or (out, lse) with lse float32
+        [n_rows, g * heads], the logarithm of the softmax's sums."""
+        w = self.worker
+        self._check_batch(batch)
+        if q.dim() != 3:
+            raise ValueError("q must be [n_rows, query heads, head_dim]")
+        if q.dtype not in (torch.float16, torch.bfloat16):
+            raise TypeError(f"q has dtype {q.dtype}, expected float16 or bfloat16")
+        n, hq = batch.n_rows, q.shape[1]
+        qv = _vectors(q, "q", q.dtype, w.device, n, hq, self.head_dim)
+        if tree is not None:
+            _need(tree, "tree", torch.int64, w.device)
+            if tree.shape != (n,) or not tree.is_contiguous():
+                raise ValueError(f"tree must be a contiguous [{n}]")
+        if out is None:
+            out = torch.empty((n, hq, self.head_dim), dtype=q.dtype, device=w.device)
+        ov = _vectors(out, "out", q.dtype, w.device, n, hq, self.head_dim)
+        sums = torch.empty((n, hq), dtype=torch.float32, device=w.device) if lse else None
+        if scale is None:
+            scale = self.head_dim ** -0.5
+        rc = w.L.orloj_worker_attend(w.w, self._ref, batch._ref, DTYPES[q.dtype], hq, scale, qv,
+                                     None if tree is None else tree.data_ptr(), ov,
+                                     None if sums is None else sums.data_ptr())
+        if rc:
+            w.ctx._check(rc)
+        return (out, sums) if lse else out
