@@ -646,7 +646,8 @@ int orloj_worker_cache_read(orloj_worker *worker, const orloj_cache *cache,
  * dtype (ORLOJ_F16 or ORLOJ_BF16) is the type of q and out.  The scores' sums,
  * the softmax's statistics and the output's sums are held in 32 bits; q, scaled
  * per row, and the weights enter the products in 16-bit floating point with 11
- * significant bits, the codes exactly.  Results are the same bits every time
+ * significant bits, the codes exactly; value scales up to 2^100 (values up to
+ * 2^106) leave the weights in that format's range.  Results are the same bits every time
  * for the same arguments.
  */
 int orloj_worker_attend(orloj_worker *worker, const orloj_cache *cache, const orloj_batch *batch,

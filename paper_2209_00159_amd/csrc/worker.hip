@@ -4,7 +4,7 @@
 //
 //   adapt_down_kernel, adapt_up_kernel   h = A_a x, then y = base + s B_a h
 //   cache_write_kernel, cache_read_kernel  keys and values <-> 8-bit pages
-//   attend_kernel                        attention of the rows over the pages
+//   attend_kernel, attend_join_kernel    attention of the rows over the pages
 
 #include <hip/hip_fp8.h>
 #include <hip/hip_runtime.h>
@@ -271,66 +271,442 @@ struct AttendArgs {
     float* lse;
     float scale;
     int q_heads, group;
+    int half;               // q and out are float16, else bfloat16
+    int q_wide, out_wide;   // vectors of 8 elements can be loaded / stored whole
+    int block_pairs;        // (row, head) pairs a workgroup takes
+    int chunk;              // tokens a workgroup takes, a multiple of 128
+    float* part_o;          // [splits][n_rows * q_heads][pad] sums, where a request is split
+    float2* part_cl;        // and their (c, l)
 };
 
-// A wave per (request, row, query head): 64 tokens at a time, a token a lane for
-// the scores, then a dimension a lane for the weighted sum.
-template <class E>
-__global__ __launch_bounds__(64) void attend_kernel(AttendArgs a) {
-    using T = typename E::T;
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
+typedef uint16_t ushort8_t __attribute__((ext_vector_type(8)));
+
+union Half8 {
+    half8_t v;
+    half2_t p[4];
+};
+
+__device__ __forceinline__ half2_t as_half2(uint32_t x) { return __builtin_bit_cast(half2_t, x); }
+
+// Two codes (bytes 0, 1 or 2, 3 of x) as 16-bit floats, exactly.  INT8: the byte
+// with its sign flipped, u = b + 128, is the low byte of the float 1024 + u.
+template <int FMT, bool HI>
+__device__ __forceinline__ half2_t two_codes(uint32_t x) {
+    if (FMT == ORLOJ_CACHE_FP8) return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, HI);
+    const half2_t bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+    return as_half2(__builtin_amdgcn_perm(0x64646464u, x, HI ? 0x04030402u : 0x04010400u)) - bias;
+}
+
+// Over the four lanes that hold one query row's column (lanes n, n + 16, ...).
+__device__ __forceinline__ float column_max(float x) {
+    uint32_t u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    u = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+    const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float column_sum(float x) {
+    x += __shfl_xor(x, 16, 64);
+    return x + __shfl_xor(x, 32, 64);
+}
+
+// Eight outputs of a vector, from dimension d on, times inv, rounded once.
+__device__ __forceinline__ void store8(const AttendArgs& a, int64_t at, int d, const float* z, float inv) {
+    uint16_t* dst = (uint16_t*)a.out.d + at + d;
+    ushort8_t h;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        h[j] = a.half ? __builtin_bit_cast(uint16_t, (_Float16)(z[j] * inv)) : __builtin_bit_cast(uint16_t, (__bf16)(z[j] * inv));
+    if (a.out_wide) {
+        if (d < a.c.dim) *(ushort8_t*)dst = h;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (d + j < a.c.dim) dst[j] = h[j];
+    }
+}
+
+// The last row of the workgroup that holds (row i, head j of its group).
+__device__ __forceinline__ int block_last_row(const AttendArgs& a, int i, int j, int rows) {
+    const int block = (i * a.group + j) / a.block_pairs;
+    return (min((block + 1) * a.block_pairs, rows * a.group) - 1) / a.group;
+}
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+
+// One tile of 32 tokens as a lane loads it: two 16-token parts of a page.
+template <int DP>
+struct Tile {
+    uint4_t k[2][DP / 64];        // token lane & 15, its dimensions (lane >> 4) DP / 4 ..
+    uint32_t v[8][DP / 64];       // tokens 4 (lane >> 4) + 0..3 of both parts, dimensions (lane & 15) DP / 16 ..
+    float4_t ks[2], vs[2];        // scales of those eight tokens
+};
+
+// out = softmax(scale q K^T) V for 16 NT (row, head) pairs that share a key head,
+// over a.chunk tokens.  Everything in base 2, relative to a reference c of the row:
+//   s = q . k scale log2 e,  p = 2^(s + c),  l = sum p,  o = sum p v,
+// so that out = o / l and lse = (log2 l - c) / log2 e whatever c was; c moves down
+// when scores or value scales outgrow it, and o and l are rescaled then.
+//   S^T = K Q^T   v_mfma_f32_16x16x32_f16, a tile's tokens by 16 rows
+//   O^T = V^T P^T the same; S^T's registers hold what P^T's operand needs
+// The order of the k index is free as long as both operands agree, so no operand
+// goes through LDS: a lane loads its share of the page rows whole (16 bytes of K,
+// DP / 16 of V a token) and the codes become 16-bit floats in registers.
+// Four waves take every fourth tile, the next one's loads in flight; their sums meet
+// in LDS.
+template <int FMT, int DP, int NT>
+__global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
+    constexpr int R = 16 * NT, ND = DP / 64, MT = DP / 16;
+    __shared__ __attribute__((aligned(16))) float o_sum[R][DP + 4];
+    __shared__ float c_of[kWaves][R], l_of[kWaves][R];
     const CacheArgs& c = a.c;
-    const int lane = threadIdx.x, r = blockIdx.z, i = blockIdx.x, qh = blockIdx.y, head = qh / a.group;
-    __shared__ float q[ORLOJ_MAX_HEAD_DIM];
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int split = blockIdx.x, head = blockIdx.y % c.heads, block = blockIdx.y / c.heads, r = blockIdx.z;
+
+    int64_t first;
+    int rows, length;
+    if (!request_of(c, r, first, rows, length)) return;
+    const int pair0 = block * R, pairs = rows * a.group;
+    if (pair0 >= pairs) return;
+    const int context = length - rows;
+    const int i_first = pair0 / a.group, i_last = (min(pair0 + R, pairs) - 1) / a.group;
+    const int end = a.tree ? length : context + i_last + 1;   // tokens any row may see
+    const int plain = a.tree ? context : context + i_first + 1; // tokens every row sees
+    const int begin = split * a.chunk, stop = min(begin + a.chunk, end);
+    if (begin >= stop && split > 0) return;
+
+    // queries: 16-bit floats relative to a power of two of their row
+    Half8 q[NT][DP / 32];
+    float f[NT];
+    int lim[NT];
+    uint64_t mask[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int pair = pair0 + 16 * t + n;
+        const int i = pair / a.group;
+        const bool live = pair < pairs;
+        const int64_t at = (first + i) * a.q.row + (int64_t)(head * a.group + pair - i * a.group) * a.q.head;
+        float x[DP / 4], amax = 0.0f;
+#pragma unroll
+        for (int e = 0; e < DP / 4; ++e) x[e] = 0.0f;
+        if (live) {
+            const uint16_t* src = (const uint16_t*)a.q.d + at;
+#pragma unroll
+            for (int e = 0; e < DP / 4; e += 8) {
+                const int d = g * (DP / 4) + e;
+                ushort8_t h = {};
+                if (a.q_wide) {
+                    if (d < c.dim) h = *(const ushort8_t*)(src + d);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (d + j < c.dim) h[j] = src[d + j];
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint16_t u = h[j];
+                    x[e + j] = a.half ? (float)__builtin_bit_cast(_Float16, u) : __builtin_bit_cast(float, (uint32_t)u << 16);
+                }
+            }
+        }
+        bool bad = false;
+#pragma unroll
+        for (int e = 0; e < DP / 4; ++e) {
+            amax = fmaxf(amax, fabsf(x[e]));
+            bad |= !(fabsf(x[e]) < INFINITY);
+        }
+        amax = column_max(bad ? INFINITY : amax);
+        bad = !(amax < INFINITY);
+        const int ex = bad || amax == 0.0f ? 0 : __builtin_amdgcn_frexp_expf(amax);
+        f[t] = bad ? NAN : ldexpf(a.scale * kLog2e, ex);
+#pragma unroll
+        for (int e = 0; e < DP / 4; ++e)
+            q[t][e / 8].v[e % 8] = (_Float16)(bad ? 0.0f : ldexpf(x[e], -ex));
+        lim[t] = live ? (a.tree ? context - 1 : context + i) : -1;
+        mask[t] = live && a.tree ? a.tree[first + i] : 0;
+    }
+
+    float4_t o[NT][MT];
+    float l[NT], ref[NT], top[NT], vlim[NT];
+    // nothing seen: a reference that any score moves
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        l[t] = 0.0f;
+        top[t] = -3e38f;      // largest score so far (of the four lanes of a column)
+        vlim[t] = 0x1p-88f;   // largest value scale its reference allows
+        ref[t] = 3e38f;
+#pragma unroll
+        for (int j = 0; j < MT; ++j) o[t][j] = float4_t{0, 0, 0, 0};
+    }
+
+    const int tiles = stop > begin ? (stop - begin + 31) >> 5 : 0;
+    const int last_part = (end - 1) >> 4;   // 16-token parts beyond it hold nothing
+    const int32_t* table = c.table + (int64_t)r * c.max_pages;
+    int page_of = 0;                        // lane 2 i + part: the page of the wave's i-th tile from the last load
+
+    auto load_pages = [&](int it) {
+        const int tile = wave + (it + (lane >> 1)) * kWaves;
+        const int part = min((begin >> 4) + 2 * tile + (lane & 1), last_part);
+        int p = table[part >> (c.shift - 4)];
+        if (p < 0 || p >= c.pages) {
+            atomicOr(c.err, kErrPage);
+            p = 0;
+        }
+        page_of = p;
+    };
+    auto load = [&](int it, Tile<DP>& x) {
+        if ((it & 31) == 0) load_pages(it);
+        const int t0 = begin + (wave + it * kWaves) * 32;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int part = min((t0 >> 4) + h, last_part);
+            const int p = __builtin_amdgcn_readlane(page_of, (2 * it + h) & 63);
+            const int64_t slot = (((int64_t)p * c.heads + head) << c.shift) + ((part << 4) & (c.page - 1));
+            const uint8_t* kp = c.k + slot * DP;
+            const uint8_t* vp = c.v + slot * DP;
+#pragma unroll
+            for (int j = 0; j < ND; ++j) x.k[h][j] = *(const uint4_t*)(kp + n * DP + g * (DP / 4) + 16 * j);
+            // tokens past the end may hold codes that no weight of zero removes (NaN): the
+            // last token instead
+            const int most = min(15, end - 1 - (part << 4));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint8_t* row = vp + min(4 * g + i, most) * DP + n * (DP / 16);
+#pragma unroll
+                for (int j = 0; j < ND; ++j) x.v[4 * h + i][j] = ((const uint32_t*)row)[j];
+            }
+            x.ks[h] = *(const float4_t*)(c.ks + slot + 4 * g);
+            x.vs[h] = *(const float4_t*)(c.vs + slot + 4 * g);
+        }
+    };
+    auto use = [&](int it, Tile<DP>& x) {
+        const int t0 = begin + (wave + it * kWaves) * 32;
+        float4_t s[NT][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) s[t][h] = float4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < DP / 32; ++e) {
+                Half8 k;
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    uint32_t u = x.k[h][e / 2][(e & 1) * 2 + w];
+                    if (FMT == ORLOJ_CACHE_INT8) u ^= 0x80808080u;
+                    k.p[2 * w] = two_codes<FMT, false>(u);
+                    k.p[2 * w + 1] = two_codes<FMT, true>(u);
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k.v, q[t][e].v, s[t][h], 0, 0, 0);
+            }
+        }
+        const bool all = t0 + 32 <= plain && t0 + 32 <= stop;
+        Half8 p[NT];
+        float big = 0.0f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) big = fmaxf(big, x.vs[h][i]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float vs[8], w[8];
+            float mx = -INFINITY, vmax = big;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                w[j] = s[t][j >> 2][j & 3] * x.ks[j >> 2][j & 3] * f[t];
+                vs[j] = x.vs[j >> 2][j & 3];
+            }
+            if (!all) {
+                vmax = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int tok = t0 + 16 * (j >> 2) + 4 * g + (j & 3);
+                    const int drafted = (int)(mask[t] >> ((tok - context) & 63)) & 1;
+                    const bool sees = (tok < stop) & ((tok <= lim[t]) | drafted);
+                    w[j] = sees ? w[j] : -INFINITY;
+                    vs[j] = sees ? vs[j] : 0.0f;
+                    vmax = fmaxf(vmax, vs[j]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) mx = fmaxf(mx, w[j]);
+            // scores up to 2^6 above the reference's, value scales up to 4 above its, so
+            // that weights of up to 2^14 fit a 16-bit float and all but those 2^-20 below
+            // the largest keep its 11 bits
+            if (__any(mx > top[t] + 6.0f || vmax > vlim[t])) {
+                top[t] = fmaxf(top[t], column_max(mx));
+                const float most = column_max(vmax);
+                if (most > vlim[t]) vlim[t] = ldexpf(1.0f, min(__builtin_amdgcn_frexp_expf(most), 100) + 2);
+                const float now = 8.0f - __builtin_amdgcn_logf(vlim[t]) - top[t];
+                const float by = __builtin_amdgcn_exp2f(now - ref[t]);
+                ref[t] = now;
+                l[t] *= by;
+#pragma unroll
+                for (int j = 0; j < MT; ++j) o[t][j] *= by;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                w[j] = __builtin_amdgcn_exp2f(w[j] + ref[t]);
+                l[t] += w[j];
+                w[j] *= vs[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p[t].v[j] = (_Float16)w[j];
+        }
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            uint32_t lo[4], hi[4];   // bytes 0, 1 and 2, 3 of two tokens each
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t u = x.v[2 * i][d], w = x.v[2 * i + 1][d];
+                if (FMT == ORLOJ_CACHE_INT8) {
+                    u ^= 0x80808080u;
+                    w ^= 0x80808080u;
+                }
+                lo[i] = __builtin_amdgcn_perm(w, u, 0x05010400u);
+                hi[i] = __builtin_amdgcn_perm(w, u, 0x07030602u);
+            }
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                Half8 v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t u = b < 2 ? lo[i] : hi[i];
+                    v.p[i] = b & 1 ? two_codes<FMT, true>(u) : two_codes<FMT, false>(u);
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    o[t][4 * d + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v.v, p[t].v, o[t][4 * d + b], 0, 0, 0);
+            }
+        }
+    };
+
+    const int mine = tiles > wave ? (tiles - wave + kWaves - 1) / kWaves : 0;
+    if (c.pages == 0) {
+        atomicOr(c.err, kErrPage);
+    } else if (mine > 0) {
+        Tile<DP> x, y;
+        load(0, x);
+        int it = 0;
+        for (; it + 2 <= mine; it += 2) {
+            load(it + 1, y);
+            use(it, x);
+            if (it + 2 < mine) load(it + 2, x);
+            use(it + 1, y);
+        }
+        if (it < mine) use(it, x);
+    }
+
+    // the four waves' sums, in turn, so that the order of the additions is fixed
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        l[t] = column_sum(l[t]);
+        if (g == 0) {
+            c_of[wave][16 * t + n] = ref[t];
+            l_of[wave][16 * t + n] = l[t];
+        }
+    }
+    __syncthreads();
+    float by[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int k = 16 * t + n;
+        by[t] = __builtin_amdgcn_exp2f(fminf(fminf(c_of[0][k], c_of[1][k]), fminf(c_of[2][k], c_of[3][k])) - ref[t]);
+    }
+    for (int w = 0; w < kWaves; ++w) {
+        if (w == wave) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float* at = &o_sum[16 * t + n][(4 * g + i) * MT];
+#pragma unroll
+                    for (int j = 0; j < MT; j += 4) {
+                        float4_t x = {o[t][j][i], o[t][j + 1][i], o[t][j + 2][i], o[t][j + 3][i]};
+                        x *= by[t];
+                        *(float4_t*)(at + j) = w ? *(float4_t*)(at + j) + x : x;
+                    }
+                }
+        }
+        __syncthreads();
+    }
+
+    const bool whole = a.chunk >= end;
+    for (int k = threadIdx.x; k < R * (DP / 8); k += kThreads) {
+        const int row = k / (DP / 8), d = k % (DP / 8) * 8, pair = pair0 + row;
+        if (pair >= pairs) break;
+        const float m = fminf(fminf(c_of[0][row], c_of[1][row]), fminf(c_of[2][row], c_of[3][row]));
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) sum += l_of[w][row] * __builtin_amdgcn_exp2f(m - c_of[w][row]);
+        const int i = pair / a.group, qh = head * a.group + pair - i * a.group;
+        const int64_t global = (first + i) * a.q_heads + qh;
+        const float4_t x = *(float4_t*)&o_sum[row][d], y = *(float4_t*)&o_sum[row][d + 4];
+        if (whole) {
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            float z[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            store8(a, (first + i) * a.out.row + (int64_t)qh * a.out.head, d, z, inv);
+            if (d == 0 && a.lse) a.lse[global] = sum == 0.0f ? -INFINITY : (__builtin_amdgcn_logf(sum) - m) * kLn2;
+        } else {
+            const int64_t at = (int64_t)split * c.rows * a.q_heads + global;
+            *(float4_t*)(a.part_o + at * DP + d) = x;
+            *(float4_t*)(a.part_o + at * DP + d + 4) = y;
+            if (d == 0) a.part_cl[at] = float2{m, sum};
+        }
+    }
+}
+
+// Joins the parts of a (row, head) pair that was split over tokens: a workgroup a pair,
+// every fourth part a wave.
+template <int DP>
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
+    constexpr int V = DP / 64;
+    __shared__ float o_sum[kWaves][DP];
+    __shared__ float l_sum[kWaves];
+    const CacheArgs& c = a.c;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int i = blockIdx.x, qh = blockIdx.y, r = blockIdx.z;
     int64_t first;
     int rows, length;
     if (!request_of(c, r, first, rows, length) || i >= rows) return;
-    const T* x = (const T*)a.q.d + (first + i) * a.q.row + qh * a.q.head;
-    for (int d = lane; d < c.dim; d += 64) q[d] = E::up(x[d]) * a.scale;
-    __syncthreads();
-    const int context = length - rows;
-    const uint64_t mask = a.tree ? a.tree[first + i] : 0;
-    float m = -INFINITY, l = 0.0f, o[4] = {};
-    const int end = a.tree ? length : context + i + 1;
-    for (int t0 = 0; t0 < end; t0 += 64) {
-        const int t = t0 + lane;
-        bool sees = t < end && (!a.tree || t < context || (mask >> (t - context) & 1));
-        int64_t slot = -1;
-        if (t < end) slot = slot_of(c, r, t, head);
-        sees = sees && slot >= 0;
-        float s = -INFINITY, w = 0.0f;
-        if (sees) {
-            const uint8_t* k = c.k + slot * c.pad;
-            float dot = 0.0f;
-            for (int d = 0; d < c.dim; ++d) dot = fmaf(q[d], from_code(c.format, k[d]), dot);
-            s = dot * c.ks[slot];
-        }
-        float top = s;
-        for (int k = 32; k; k >>= 1) {
-            const float other = __shfl_xor(top, k, 64);
-            top = other > top || other != other ? other : top;
-        }
-        top = m > top ? m : top;
-        if (top == -INFINITY) continue;
-        const float keep = __expf(m - top);
-        if (sees) w = expf(s - top);
-        m = top;
-        float sum = w;
-        for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k, 64);
-        l = l * keep + sum;
-        for (int j = 0; j < 4; ++j) o[j] *= keep;
-        for (int k = 0; k < 64; ++k) {
-            if (!__shfl((int)sees, k, 64)) continue;
-            const float p = __shfl(w, k, 64);
-            const int64_t at = __shfl(slot, k, 64);
-            const float pv = p * c.vs[at];
-            for (int j = 0; j < 4; ++j)
-                if (lane + 64 * j < c.dim) o[j] = fmaf(pv, from_code(c.format, c.v[at * c.pad + lane + 64 * j]), o[j]);
-        }
+    // the tokens the row's workgroup saw: those of its block's last row
+    const int end = a.tree ? length : length - rows + block_last_row(a, i, qh % a.group, rows) + 1;
+    if (a.chunk >= end) return;
+    const int parts = (end + a.chunk - 1) / a.chunk;
+    const int64_t stride = c.rows * a.q_heads, global = (first + i) * a.q_heads + qh;
+    float m = 3e38f;
+    for (int k = lane; k < parts; k += 64) m = fminf(m, a.part_cl[k * stride + global].x);
+    for (int k = 32; k; k >>= 1) m = fminf(m, __shfl_xor(m, k, 64));
+    float o[V] = {}, l = 0.0f;
+#pragma unroll 4
+    for (int k = wave; k < parts; k += kWaves) {
+        const float2 cl = a.part_cl[k * stride + global];
+        const float by = __builtin_amdgcn_exp2f(m - cl.x);
+        const float* src = a.part_o + (k * stride + global) * DP + lane * V;
+        l = fmaf(cl.y, by, l);
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[j] = fmaf(src[j], by, o[j]);
     }
-    T* y = (T*)a.out.d + (first + i) * a.out.row + qh * a.out.head;
-    for (int j = 0; j < 4; ++j)
-        if (lane + 64 * j < c.dim) y[lane + 64 * j] = E::down(l != 0.0f ? o[j] / l : 0.0f);
-    if (a.lse && lane == 0) a.lse[(first + i) * a.q_heads + qh] = l != 0.0f ? m + logf(l) : -INFINITY;
+#pragma unroll
+    for (int j = 0; j < V; ++j) o_sum[wave][lane * V + j] = o[j];
+    if (lane == 0) l_sum[wave] = l;
+    __syncthreads();
+    const float sum = (l_sum[0] + l_sum[1]) + (l_sum[2] + l_sum[3]);
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int d = threadIdx.x * 8;
+    if (d < DP) {
+        float z[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = (o_sum[0][d + j] + o_sum[1][d + j]) + (o_sum[2][d + j] + o_sum[3][d + j]);
+        store8(a, (first + i) * a.out.row + (int64_t)qh * a.out.head, d, z, inv);
+        if (d == 0 && a.lse) a.lse[global] = sum == 0.0f ? -INFINITY : (__builtin_amdgcn_logf(sum) - m) * kLn2;
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -459,6 +835,57 @@ int cache_copy(orloj_worker* w, const orloj_cache* cache, const orloj_batch* bat
     return launch(w, "cache_read_kernel", kernel, g, kThreads, c, kv, vv);
 }
 
+// Whether 8 elements of 16 bits can be moved as one: every vector starts on 16 bytes.
+bool wide(const Vectors& v, int dim) {
+    return ((uintptr_t)v.d & 15) == 0 && v.row % 8 == 0 && v.head % 8 == 0 && dim % 8 == 0;
+}
+
+template <int FMT, int DP, int NT>
+int attend_tiles(orloj_worker* w, AttendArgs& a) {
+    const int64_t pairs = (int64_t)a.c.max_rows * a.group, blocks = (pairs + 16 * NT - 1) / (16 * NT);
+    a.block_pairs = 16 * NT;
+    const int64_t groups = (int64_t)a.c.requests * a.c.heads * blocks;
+    // Eight workgroups a unit where there are fewer, from at least 256 tokens each
+    const int64_t want = (8 * (int64_t)w->ctx->n_cu + groups - 1) / groups;
+    const int64_t most = std::max<int64_t>(1, (a.c.max_length + 255) / 256);
+    const int64_t splits0 = std::min(want, most);
+    a.chunk = (int)(((a.c.max_length + splits0 - 1) / splits0 + 127) / 128 * 128);
+    a.chunk = std::max(a.chunk, 128);
+    const int splits = std::max(1, (a.c.max_length + a.chunk - 1) / a.chunk);
+    if (blocks * a.c.heads > 65535)
+        return orloj_ctx_fail(w->ctx, ORLOJ_E_UNSUPPORTED, "%lld (row, head) pairs of one request are too many",
+                              (long long)(pairs * a.c.heads));
+    if (splits > 1) {
+        const size_t n = (size_t)splits * a.c.rows * a.q_heads;
+        void* p;
+        if (int rc = scratch(w, n * (DP + 2) * sizeof(float), &p)) return rc;
+        a.part_o = (float*)p;
+        a.part_cl = (float2*)(a.part_o + n * DP);
+    }
+    const dim3 grid(splits, (unsigned)(blocks * a.c.heads), a.c.requests);
+    if (int rc = launch(w, "attend_kernel", attend_kernel<FMT, DP, NT>, grid, kThreads, a)) return rc;
+    if (splits == 1) return ORLOJ_OK;
+    return launch(w, "attend_join_kernel", attend_join_kernel<DP>, dim3(a.c.max_rows, a.q_heads, a.c.requests), kThreads, a);
+}
+
+template <int FMT>
+int attend(orloj_worker* w, AttendArgs& a) {
+    const int64_t pairs = (int64_t)a.c.max_rows * a.group;
+    const int tiles = pairs <= 16 ? 1 : pairs <= 32 || a.c.pad > 128 ? 2 : 4;
+    switch (a.c.pad / 64 * 8 + tiles) {
+        case 9: return attend_tiles<FMT, 64, 1>(w, a);
+        case 10: return attend_tiles<FMT, 64, 2>(w, a);
+        case 12: return attend_tiles<FMT, 64, 4>(w, a);
+        case 17: return attend_tiles<FMT, 128, 1>(w, a);
+        case 18: return attend_tiles<FMT, 128, 2>(w, a);
+        case 20: return attend_tiles<FMT, 128, 4>(w, a);
+        case 25: return attend_tiles<FMT, 192, 1>(w, a);
+        case 26: return attend_tiles<FMT, 192, 2>(w, a);
+        case 33: return attend_tiles<FMT, 256, 1>(w, a);
+        default: return attend_tiles<FMT, 256, 2>(w, a);
+    }
+}
+
 }  // namespace
 
 extern "C" {
@@ -585,8 +1012,10 @@ int orloj_worker_attend(orloj_worker* w, const orloj_cache* cache, const orloj_b
     a.scale = scale;
     a.q_heads = n_q_heads;
     a.group = n_q_heads / a.c.heads;
-    const dim3 g(a.c.max_rows, n_q_heads, a.c.requests);
-    return launch(w, "attend_kernel", dtype == ORLOJ_F16 ? attend_kernel<F16> : attend_kernel<BF16>, g, 64, a);
+    a.half = dtype == ORLOJ_F16;
+    a.q_wide = wide(a.q, a.c.dim);
+    a.out_wide = wide(a.out, a.c.dim);
+    return a.c.format == ORLOJ_CACHE_INT8 ? attend<ORLOJ_CACHE_INT8>(w, a) : attend<ORLOJ_CACHE_FP8>(w, a);
 }
 
 }  // extern "C"
