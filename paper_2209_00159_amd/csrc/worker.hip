@@ -2,7 +2,8 @@
 // operators of a text model's step that depend on which requests the scheduler
 // put together.
 //
-//   adapt_down_kernel, adapt_up_kernel   h = A_a x, then y = base + s B_a h
+//   adapt_down_kernel, adapt_up_kernel   h = A_a x, then y = base + s B_a h (and forms
+//                                        for few rows and narrow inputs)
 //   cache_write_kernel, cache_read_kernel  keys and values <-> 8-bit pages
 //   attend_kernel, attend_join_kernel    attention of the rows over the pages
 
@@ -43,6 +44,15 @@ constexpr float kTiny = 0x1p-100f;   // vectors below this are stored as zeros
 // ---------------------------------------------------------------------------
 // element types
 // ---------------------------------------------------------------------------
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf8_t __attribute__((ext_vector_type(8)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
+typedef uint16_t ushort8_t __attribute__((ext_vector_type(8)));
+// the same at any element's address: the hardware's wide loads and stores need no alignment
+typedef ushort8_t ushort8_u __attribute__((aligned(2)));
+
 struct F32 {
     using T = float;
     static __device__ __forceinline__ float up(T x) { return x; }
@@ -50,11 +60,19 @@ struct F32 {
 };
 struct F16 {
     using T = _Float16;
+    static constexpr bool kNarrow = true;    // its range is smaller than a float's
+    static __device__ __forceinline__ float4_t mfma(ushort8_t a, ushort8_t b, float4_t c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+    }
     static __device__ __forceinline__ float up(T x) { return (float)x; }
     static __device__ __forceinline__ T down(float x) { return (T)x; }
 };
 struct BF16 {
     using T = __bf16;
+    static constexpr bool kNarrow = false;
+    static __device__ __forceinline__ float4_t mfma(ushort8_t a, ushort8_t b, float4_t c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8_t, a), __builtin_bit_cast(bf8_t, b), c, 0, 0, 0);
+    }
     static __device__ __forceinline__ float up(T x) { return (float)x; }
     static __device__ __forceinline__ T down(float x) { return (T)x; }
 };
@@ -69,13 +87,16 @@ struct AdaptArgs {
     void* y;
     const float* scale;
     const int32_t *ranks, *adapter;
-    float* h;        // [rows][rank]
+    float* h;        // [splits][rows][rank], each split's share of A x
+    int splits;      // of d_in
+    int k_part;      // elements of d_in a split takes, a multiple of 256
+    int blocks;      // blocks of outputs a workgroup takes
     int* err;
 };
 
-// Row t's adapter and its rank (0: none).
+// Row t's adapter, -1 where it has none or one of rank 0.
 __device__ __forceinline__ int adapter_of(const AdaptArgs& a, int64_t t, int& rank) {
-    int id = a.adapter[t];
+    int id = t < a.rows ? a.adapter[t] : -1;
     rank = 0;
     if (id < -1 || id >= a.n) {
         atomicOr(a.err, kErrAdapter);
@@ -88,44 +109,395 @@ __device__ __forceinline__ int adapter_of(const AdaptArgs& a, int64_t t, int& ra
             rank = min(max(rank, 0), a.rank);
         }
     }
-    return id;
+    return rank ? id : -1;
 }
 
-// One workgroup per row, a wave per rank in turn: h[t][r] = A_a[r] . x_t.
-template <class E>
-__global__ __launch_bounds__(kThreads) void adapt_down_kernel(AdaptArgs a) {
-    using T = typename E::T;
-    const int64_t t = blockIdx.x;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Where the eight elements from `start` on of a vector of `size` are loaded from: an
+// operand's last piece begins early enough to end with the vector, and the elements
+// before `start`, which an earlier piece has, count as zeros.  Both operands of a
+// product agree on that, so its order of k does not matter.
+__device__ __forceinline__ int piece_at(int start, int size) { return max(min(start, size - 8), 0); }
+
+__device__ __forceinline__ ushort8_t cut_piece(ushort8_t v, int at, int start, int size) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = at + j >= start && at + j < size ? v[j] : (uint16_t)0;
+    return v;
+}
+
+// h = A_a x for 16 NT rows and up to 16 RT ranks: D = A_a X^T, ranks by rows, on
+// v_mfma_f32_16x16x32.  Both operands are contiguous along k, so a lane loads its
+// 16 bytes of each straight into the operand's registers (32 bytes a row and lane and
+// step of 64).  The four waves take 64 of each 256 elements; their sums meet in LDS,
+// those of the splits of d_in in adapt_up_kernel.
+// The rows' distinct adapters: with NT = 1 (few rows) the z-th of the grid's z-th
+// workgroup, else one after the other (rows of a prompt share theirs).
+template <class E, int RT, int NT>
+__global__ __launch_bounds__(kThreads, RT * NT <= 16 ? 2 : 1) void adapt_down_kernel(AdaptArgs a) {
+    constexpr int ROWS = 16 * NT, RANKS = 16 * RT;
+    __shared__ __attribute__((aligned(16))) float sum[ROWS][RANKS + 4];
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t t0 = (int64_t)blockIdx.x * ROWS;
     int rank;
-    const int id = adapter_of(a, t, rank);
-    const T* x = (const T*)a.x + t * a.xs;
-    for (int r = wave; r < rank; r += kWaves) {
-        const T* w = (const T*)a.down + ((int64_t)id * a.rank + r) * a.d_in;
-        float s = 0.0f;
-        for (int k = lane; k < a.d_in; k += 64) s = fmaf(E::up(w[k]), E::up(x[k]), s);
-        for (int m = 32; m; m >>= 1) s += __shfl_xor(s, m, 64);
-        if (lane == 0) a.h[t * a.rank + r] = s;
+    const int id = adapter_of(a, lane < ROWS ? t0 + lane : a.rows, rank);
+    uint64_t left = __ballot(id >= 0);
+    for (int z = 0; left; ++z) {
+        const int lead = __builtin_ctzll(left);
+        const int which = __builtin_amdgcn_readlane(id, lead);
+        const uint64_t mine = __ballot(id == which);
+        left &= ~mine;
+        if (NT == 1 && z != (int)blockIdx.z) continue;
+        const int ranks = __builtin_amdgcn_readlane(rank, lead);
+        const uint16_t* w = (const uint16_t*)a.down + (int64_t)which * a.rank * a.d_in;
+        const int from = blockIdx.y * a.k_part, to = min(from + a.k_part, a.d_in);
+
+        const uint16_t *ap[RT], *xp[NT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) ap[i] = w + (int64_t)min(16 * i + n, ranks - 1) * a.d_in;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) xp[j] = (const uint16_t*)a.x + min(t0 + 16 * j + n, a.rows - 1) * a.xs;
+        float4_t acc[RT][NT] = {};
+        ushort8_t av[2][RT], xv[2][NT];
+        auto load = [&](int k, int s) {
+            const int at = k + 16 * g + 8 * s;
+#pragma unroll
+            for (int i = 0; i < RT; ++i) av[s][i] = *(const ushort8_u*)(ap[i] + at);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) xv[s][j] = *(const ushort8_u*)(xp[j] + at);
+        };
+        auto use = [&](int s) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = E::mfma(av[s][i], xv[s][j], acc[i][j]);
+        };
+        const int full = min(to, a.d_in - 63);      // steps that begin below it are whole
+        int k = from + 64 * wave;
+        if (k < full) {
+            load(k, 0);
+            load(k, 1);
+        }
+        for (; k < full; k += 256) {
+            use(0);
+            if (k + 256 < full) load(k + 256, 0);
+            use(1);
+            if (k + 256 < full) load(k + 256, 1);
+        }
+        if (k < to) {
+#pragma unroll 1
+            for (int s = 0; s < 2; ++s) {
+                const int start = k + 16 * g + 8 * s, at = piece_at(start, a.d_in);
+                ushort8_t x[NT];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) x[j] = cut_piece(*(const ushort8_u*)(xp[j] + at), at, start, a.d_in);
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    const ushort8_t v = cut_piece(*(const ushort8_u*)(ap[i] + at), at, start, a.d_in);
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[i][j] = E::mfma(v, x[j], acc[i][j]);
+                }
+            }
+        }
+        for (int v = 0; v < kWaves; ++v) {
+            if (v == wave) {
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        float4_t* at = (float4_t*)&sum[16 * j + n][16 * i + 4 * g];
+                        *at = v ? *at + acc[i][j] : acc[i][j];
+                    }
+            }
+            __syncthreads();
+        }
+        float* h = a.h + ((int64_t)blockIdx.y * a.rows + t0) * a.rank;
+        for (int e = threadIdx.x; e < ROWS * a.rank; e += kThreads) {
+            const int row = e / a.rank, r = e - row * a.rank;
+            if (mine >> row & 1) h[e] = r < ranks ? sum[row][r] : 0.0f;
+        }
+        __syncthreads();
     }
 }
 
-// A thread per output element.
+// h of a d_in below 8, the width of the operands' loads: a thread each.
 template <class E>
-__global__ __launch_bounds__(kThreads) void adapt_up_kernel(AdaptArgs a) {
-    using T = typename E::T;
-    const int64_t t = blockIdx.x;
-    const int o = blockIdx.y * kThreads + threadIdx.x;
-    if (o >= a.d_out) return;
+__global__ __launch_bounds__(kThreads) void adapt_down_narrow_kernel(AdaptArgs a) {
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, t = i / a.rank;
+    const int r = (int)(i - t * a.rank);
     int rank;
     const int id = adapter_of(a, t, rank);
+    if (id < 0) return;
+    const typename E::T* w = (const typename E::T*)a.down + ((int64_t)id * a.rank + r) * a.d_in;
+    const typename E::T* x = (const typename E::T*)a.x + t * a.xs;
     float s = 0.0f;
-    if (rank) {
-        const T* w = (const T*)a.up + ((int64_t)id * a.d_out + o) * a.rank;
-        for (int r = 0; r < rank; ++r) s = fmaf(E::up(w[r]), a.h[t * a.rank + r], s);
-        if (a.scale) s *= a.scale[id];
+    if (r < rank)
+        for (int k = 0; k < a.d_in; ++k) s = fmaf(E::up(w[k]), E::up(x[k]), s);
+    a.h[i] = s;
+}
+
+// Row t's h, summed over the splits, as two 16-bit floats each (high and low part, so
+// that it keeps 16 bits or more) times a power of two that keeps float16's range, in the
+// order that load_up's pieces have: 16 lanes a row, places n, n + 16, ...
+template <class E, int STEPS>
+__device__ __forceinline__ void put_h(const AdaptArgs& a, int64_t t, bool live, uint16_t* hi_at, uint16_t* lo_at, float* by) {
+    const int n = threadIdx.x & 15;
+    float v[2 * STEPS] = {};
+    if (live) {
+        const float* h = a.h + t * a.rank;
+        int r[2 * STEPS];
+        bool has[2 * STEPS];
+#pragma unroll
+        for (int j = 0; j < 2 * STEPS; ++j) {
+            const int start = (n & 8) + 16 * j;
+            r[j] = min(piece_at(start, a.rank) + (n & 7), a.rank - 1);
+            has[j] = r[j] >= start && piece_at(start, a.rank) + (n & 7) < a.rank;
+        }
+#pragma unroll 8
+        for (int s = 0; s < a.splits; ++s, h += a.rows * a.rank)
+#pragma unroll
+            for (int j = 0; j < 2 * STEPS; ++j) v[j] += has[j] ? h[r[j]] : 0.0f;
     }
-    if (a.base) s += E::up(((const T*)a.base)[t * a.bs + o]);
-    ((T*)a.y)[t * a.ys + o] = E::down(s);
+    int ex = 0;
+    if (E::kNarrow) {
+        float amax = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 2 * STEPS; ++j) amax = fmaxf(amax, fabsf(v[j]));
+        for (int m = 8; m; m >>= 1) amax = fmaxf(amax, __shfl_xor(amax, m, 64));
+        ex = amax > 0.0f && amax < INFINITY ? __builtin_amdgcn_frexp_expf(amax) : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < 2 * STEPS; ++j) {
+        const float x = ldexpf(v[j], -ex);
+        const typename E::T hi = E::down(x);
+        const float low = x - E::up(hi);
+        const typename E::T lo = E::down(low == low ? low : 0.0f);   // inf - inf
+        hi_at[n + 16 * j] = __builtin_bit_cast(uint16_t, hi);
+        lo_at[n + 16 * j] = __builtin_bit_cast(uint16_t, lo);
+    }
+    if (n == 0) *by = ldexpf(1.0f, ex);
+}
+
+// The operand of 64 outputs from o0 on: row m of product j is output 16 (m / 4) + 4 j +
+// m mod 4, so that a lane of the result holds 16 adjacent outputs of a row.
+template <int STEPS>
+__device__ __forceinline__ void load_up(const AdaptArgs& a, int which, int ranks, int o0, ushort8_t (&wv)[STEPS][4]) {
+    const int n = threadIdx.x & 15, g = threadIdx.x >> 4 & 3;
+    const uint16_t* w = (const uint16_t*)a.up + (int64_t)which * a.d_out * a.rank;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+        const int o = min(o0 + 16 * (n >> 2) + 4 * m + (n & 3), a.d_out - 1);
+#pragma unroll
+        for (int e = 0; e < STEPS; ++e) {
+            const uint16_t* p = w + (int64_t)o * a.rank;
+            if (STEPS > 1 || a.rank >= 8) {
+                wv[e][m] = *(const ushort8_u*)(p + piece_at(32 * e + 8 * g, a.rank));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) wv[e][m][j] = p[min(j, a.rank - 1)];
+            }
+        }
+    }
+    // columns past the adapter's rank may hold anything
+    if (ranks < a.rank || a.rank < 8) {
+#pragma unroll
+        for (int e = 0; e < STEPS; ++e)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) wv[e][m] = cut_piece(wv[e][m], piece_at(32 * e + 8 * g, a.rank), 0, ranks);
+    }
+}
+
+template <class E, int STEPS>
+__device__ __forceinline__ void product_up(const ushort8_t (&wv)[STEPS][4], const uint16_t* hi_at, const uint16_t* lo_at, float4_t (&d)[4]) {
+    const int g = threadIdx.x >> 4 & 3;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) d[m] = float4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < STEPS; ++e) {
+        const ushort8_t hi = *(const ushort8_t*)(hi_at + 32 * e + 8 * g), lo = *(const ushort8_t*)(lo_at + 32 * e + 8 * g);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            d[m] = E::mfma(wv[e][m], lo, d[m]);
+            d[m] = E::mfma(wv[e][m], hi, d[m]);
+        }
+    }
+}
+
+// A lane's 16 outputs of a row, as two pieces; element by element in the last block of a
+// width that 64 does not divide.
+template <bool FULL>
+__device__ __forceinline__ void load_base(const AdaptArgs& a, int64_t t, int o0, ushort8_t (&v)[2]) {
+    const int o = o0 + (threadIdx.x >> 4 & 3) * 16;
+    v[0] = v[1] = ushort8_t{0, 0, 0, 0, 0, 0, 0, 0};
+    if (!a.base || t >= a.rows) return;
+    const uint16_t* p = (const uint16_t*)a.base + t * a.bs;
+    if (FULL) {
+        v[0] = *(const ushort8_u*)(p + o);
+        v[1] = *(const ushort8_u*)(p + o + 8);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i >> 3][i & 7] = p[min(o + i, a.d_out - 1)];
+    }
+}
+
+template <class E, bool FULL>
+__device__ __forceinline__ void put_y(const AdaptArgs& a, int64_t t, int o0, const float4_t (&d)[4], float f, const ushort8_t (&v)[2]) {
+    const int o = o0 + (threadIdx.x >> 4 & 3) * 16;
+    uint16_t* y = (uint16_t*)a.y + t * a.ys;
+    ushort8_t z[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const uint16_t u = v[i >> 3][i & 7];
+        const float x = fmaf(d[i >> 2][i & 3], f, E::up(__builtin_bit_cast(typename E::T, u)));
+        z[i >> 3][i & 7] = __builtin_bit_cast(uint16_t, E::down(x));
+    }
+    if (FULL) {
+        *(ushort8_u*)(y + o) = z[0];
+        *(ushort8_u*)(y + o + 8) = z[1];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (o + i < a.d_out) y[o + i] = z[i >> 3][i & 7];
+    }
+}
+
+// y = base + s B_a h: D = B_a H^T, outputs by rows.  A row is written from the product
+// with its own adapter, so a weight that is not finite stays with the rows that use it.
+//
+// Few rows: 16 a workgroup and 64 outputs, every fourth distinct adapter a wave.  What
+// costs is the chain of loads, so those that do not wait for h go first: the bases and
+// the weights of the wave's first PRE adapters.
+template <class E, int STEPS, bool FULL>
+__device__ __forceinline__ void up_few(const AdaptArgs& a, int o0) {
+    constexpr int PITCH = 32 * STEPS + 8, PRE = 4 / STEPS;
+    __shared__ __attribute__((aligned(16))) uint16_t hs[2][16][PITCH];
+    __shared__ float by[16];
+    const int lane = threadIdx.x & 63, n = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t t0 = (int64_t)blockIdx.y * 16;
+    int rank;
+    const int id = adapter_of(a, lane < 16 ? t0 + lane : a.rows, rank);
+    const uint64_t some = __ballot(id >= 0);
+
+    ushort8_t base[2];
+    load_base<FULL>(a, t0 + n, o0, base);
+    uint64_t left = some;
+    int skip = wave;                  // distinct adapters before the wave's next
+    uint64_t mine[PRE];               // rows of the wave's next adapters
+    float s[PRE];
+    ushort8_t wv[PRE][STEPS][4];
+    auto next = [&]() {
+#pragma unroll
+        for (int p = 0; p < PRE; ++p) {
+            mine[p] = 0;
+            for (; left; --skip) {
+                const int lead = __builtin_ctzll(left), which = __builtin_amdgcn_readlane(id, lead);
+                const uint64_t rows = __ballot(id == which);
+                left &= ~rows;
+                if (skip == 0) {
+                    mine[p] = rows;
+                    s[p] = a.scale ? a.scale[which] : 1.0f;
+                    load_up<STEPS>(a, which, __builtin_amdgcn_readlane(rank, lead), o0, wv[p]);
+                    skip = kWaves - 1;
+                    break;
+                }
+            }
+        }
+    };
+    next();
+    const int row = threadIdx.x >> 4;
+    put_h<E, STEPS>(a, t0 + row, some >> row & 1, hs[0][row], hs[1][row], &by[row]);
+    __syncthreads();
+    float4_t d[4];
+    while (mine[0]) {
+#pragma unroll
+        for (int p = 0; p < PRE; ++p) {
+            if (!mine[p]) continue;
+            product_up<E, STEPS>(wv[p], hs[0][n], hs[1][n], d);
+            if (mine[p] >> n & 1) put_y<E, FULL>(a, t0 + n, o0, d, s[p] * by[n], base);
+        }
+        next();
+    }
+    if (wave == 0 && !(some >> n & 1) && t0 + n < a.rows) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m) d[m] = float4_t{0, 0, 0, 0};
+        put_y<E, FULL>(a, t0 + n, o0, d, 0.0f, base);
+    }
+}
+
+template <class E, int STEPS>
+__global__ __launch_bounds__(kThreads) void adapt_up_few_kernel(AdaptArgs a) {
+    const int o0 = blockIdx.x * 64;
+    if (o0 + 64 <= a.d_out) up_few<E, STEPS, true>(a, o0);
+    else up_few<E, STEPS, false>(a, o0);
+}
+
+// Many rows: 64 a workgroup, 64 outputs a wave of each block of 256; the rows' distinct
+// adapters (adjacent rows of a prompt share theirs) one after the other.
+template <class E, int STEPS>
+__global__ __launch_bounds__(kThreads) void adapt_up_kernel(AdaptArgs a) {
+    constexpr int PITCH = 32 * STEPS + 8;
+    __shared__ __attribute__((aligned(16))) uint16_t hs[2][64][PITCH];
+    __shared__ float by[64];
+    const int lane = threadIdx.x & 63, n = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t t0 = (int64_t)blockIdx.y * 64;
+    int rank;
+    const int id = adapter_of(a, t0 + lane, rank);
+    const uint64_t some = __ballot(id >= 0);
+    for (int row = threadIdx.x >> 4; row < 64; row += kThreads / 16)
+        put_h<E, STEPS>(a, t0 + row, some >> row & 1, hs[0][row], hs[1][row], &by[row]);
+    __syncthreads();
+
+    for (int b = 0; b < a.blocks; ++b) {
+        const int o0 = (blockIdx.x * a.blocks + b) * 256 + 64 * wave;
+        if (o0 >= a.d_out) break;
+        const bool whole = o0 + 64 <= a.d_out;
+        for (uint64_t left = some; left;) {
+            const int lead = __builtin_ctzll(left), which = __builtin_amdgcn_readlane(id, lead);
+            const uint64_t mine = __ballot(id == which);
+            left &= ~mine;
+            const float s = a.scale ? a.scale[which] : 1.0f;
+            ushort8_t wv[STEPS][4];
+            load_up<STEPS>(a, which, __builtin_amdgcn_readlane(rank, lead), o0, wv);
+            if (whole) {
+                ushort8_t base[4][2];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) load_base<true>(a, t0 + 16 * j + n, o0, base[j]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (!(mine >> (16 * j) & 0xffff)) continue;
+                    float4_t d[4];
+                    product_up<E, STEPS>(wv, hs[0][16 * j + n], hs[1][16 * j + n], d);
+                    if (mine >> (16 * j + n) & 1) put_y<E, true>(a, t0 + 16 * j + n, o0, d, s * by[16 * j + n], base[j]);
+                }
+            } else {
+#pragma unroll 1
+                for (int j = 0; j < 4; ++j) {
+                    if (!(mine >> (16 * j) & 0xffff)) continue;
+                    ushort8_t base[2];
+                    load_base<false>(a, t0 + 16 * j + n, o0, base);
+                    float4_t d[4];
+                    product_up<E, STEPS>(wv, hs[0][16 * j + n], hs[1][16 * j + n], d);
+                    if (mine >> (16 * j + n) & 1) put_y<E, false>(a, t0 + 16 * j + n, o0, d, s * by[16 * j + n], base);
+                }
+            }
+        }
+        // rows without an adapter
+#pragma unroll 1
+        for (int j = 0; j < 4; ++j) {
+            const int64_t t = t0 + 16 * j + n;
+            if ((some >> (16 * j + n) & 1) || t >= a.rows) continue;
+            const float4_t none[4] = {};
+            ushort8_t base[2];
+            if (whole) {
+                load_base<true>(a, t, o0, base);
+                put_y<E, true>(a, t, o0, none, 0.0f, base);
+            } else {
+                load_base<false>(a, t, o0, base);
+                put_y<E, false>(a, t, o0, none, 0.0f, base);
+            }
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -205,9 +577,15 @@ struct Vectors {
     int64_t row, head;
 };
 
+struct CopyArgs {
+    CacheArgs c;
+    Vectors k, v;
+};
+
 // 16 lanes a vector, 16 vectors a workgroup.
 template <class E>
-__global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheArgs c, Vectors k, Vectors v) {
+__global__ __launch_bounds__(kThreads) void cache_write_kernel(CopyArgs a) {
+    const CacheArgs& c = a.c;
     using T = typename E::T;
     const int sub = threadIdx.x & 15;
     const int64_t i = (int64_t)blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
@@ -219,12 +597,12 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheArgs c, Vect
     if (!place_of_row(c, row, req, pos)) return;
     const int64_t slot = slot_of(c, req, pos, head);
     if (slot < 0) return;
-    const Vectors& from = which < c.heads ? k : v;
+    const Vectors& from = which < c.heads ? a.k : a.v;
     const T* x = (const T*)from.d + row * from.row + head * from.head;
     float amax = 0.0f;
     for (int d = sub; d < c.dim; d += 16) {
-        const float a = fabsf(E::up(x[d]));
-        amax = a > amax || a != a ? a : amax;
+        const float y = fabsf(E::up(x[d]));
+        amax = y > amax || y != y ? y : amax;
     }
     for (int m = 8; m; m >>= 1) {
         const float o = __shfl_xor(amax, m, 64);
@@ -242,7 +620,8 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CacheArgs c, Vect
 }
 
 template <class E>
-__global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheArgs c, Vectors k, Vectors v) {
+__global__ __launch_bounds__(kThreads) void cache_read_kernel(CopyArgs a) {
+    const CacheArgs& c = a.c;
     using T = typename E::T;
     const int sub = threadIdx.x & 15;
     const int64_t i = (int64_t)blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
@@ -254,7 +633,7 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheArgs c, Vecto
     if (!place_of_row(c, row, req, pos)) return;
     const int64_t slot = slot_of(c, req, pos, head);
     if (slot < 0) return;
-    const Vectors& to = which < c.heads ? k : v;
+    const Vectors& to = which < c.heads ? a.k : a.v;
     T* x = (T*)to.d + row * to.row + head * to.head;
     const uint8_t* code = (which < c.heads ? c.k : c.v) + slot * c.pad;
     const float s = (which < c.heads ? c.ks : c.vs)[slot];
@@ -279,11 +658,6 @@ struct AttendArgs {
     float2* part_cl;        // and their (c, l)
 };
 
-typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
-typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
-typedef float float4_t __attribute__((ext_vector_type(4)));
-typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
-typedef uint16_t ushort8_t __attribute__((ext_vector_type(8)));
 
 union Half8 {
     half8_t v;
@@ -760,11 +1134,53 @@ int scratch(orloj_worker* w, size_t bytes, void** out) {
 }
 
 // The launch's own status: the runtime's last error may be another library's.
-template <class... A>
-int launch(orloj_worker* w, const char* what, void (*kernel)(A...), dim3 grid, int threads, A... args) {
-    void* p[] = {(void*)&args...};
+template <class Args>
+int launch(orloj_worker* w, const char* what, void (*kernel)(Args), dim3 grid, int threads, const Args& args) {
+    void* p[] = {(void*)&args};
     const hipError_t e = hipLaunchKernel((const void*)kernel, grid, dim3(threads), p, 0, w->ctx->stream);
     return e == hipSuccess ? ORLOJ_OK : hip_err(w->ctx, e, what);
+}
+
+template <class E, int RT, int NT>
+int adapt_tiles(orloj_worker* w, AdaptArgs& a) {
+    const int tiles = (int)((a.rows + 16 * NT - 1) / (16 * NT));
+    const int slots = NT == 1 ? (int)std::min<int64_t>(std::min<int64_t>(16, a.rows), std::max(a.n, 1)) : 1;
+    // enough splits of d_in for four workgroups a unit, at least 256 elements each: a
+    // wave's step
+    const int want = (4 * w->ctx->n_cu + tiles * slots - 1) / (tiles * slots);
+    const int parts = std::min(want, (a.d_in + 255) / 256);
+    a.k_part = ((a.d_in + parts - 1) / parts + 255) / 256 * 256;
+    a.splits = (a.d_in + a.k_part - 1) / a.k_part;
+    void* h;
+    if (int rc = scratch(w, (size_t)a.splits * a.rows * a.rank * sizeof(float), &h)) return rc;
+    a.h = (float*)h;
+    const int rc = a.d_in < 8 ? launch(w, "adapt_down_narrow_kernel", adapt_down_narrow_kernel<E>,
+                                       dim3((unsigned)((a.rows * a.rank + kThreads - 1) / kThreads)), kThreads, a)
+                              : launch(w, "adapt_down_kernel", adapt_down_kernel<E, RT, NT>,
+                                       dim3(tiles, a.splits, slots), kThreads, a);
+    if (rc) return rc;
+    constexpr int STEPS = RT == 8 ? 4 : RT == 4 ? 2 : 1;
+    if (NT == 1)
+        return launch(w, "adapt_up_few_kernel", adapt_up_few_kernel<E, STEPS>, dim3((a.d_out + 63) / 64, tiles), kThreads, a);
+    const int blocks = (a.d_out + 255) / 256;
+    a.blocks = std::max(1, std::min(2, tiles * blocks / (2 * w->ctx->n_cu)));
+    return launch(w, "adapt_up_kernel", adapt_up_kernel<E, STEPS>, dim3((blocks + a.blocks - 1) / a.blocks, tiles), kThreads, a);
+}
+
+template <class E>
+int adapt(orloj_worker* w, AdaptArgs& a) {
+    // few rows: 16 a workgroup, their adapters side by side; many: 64, one adapter after
+    // the other
+    if (a.rows <= 256) {
+        if (a.rank <= 16) return adapt_tiles<E, 1, 1>(w, a);
+        if (a.rank <= 32) return adapt_tiles<E, 2, 1>(w, a);
+        if (a.rank <= 64) return adapt_tiles<E, 4, 1>(w, a);
+        return adapt_tiles<E, 8, 1>(w, a);
+    }
+    if (a.rank <= 16) return adapt_tiles<E, 1, 4>(w, a);
+    if (a.rank <= 32) return adapt_tiles<E, 2, 4>(w, a);
+    if (a.rank <= 64) return adapt_tiles<E, 4, 4>(w, a);
+    return adapt_tiles<E, 8, 4>(w, a);
 }
 
 int cache_args(orloj_worker* w, const orloj_cache* c, const orloj_batch* b, CacheArgs* a) {
@@ -811,11 +1227,11 @@ int vectors(orloj_worker* w, const orloj_vectors* v, int64_t rows, const char* n
 int cache_copy(orloj_worker* w, const orloj_cache* cache, const orloj_batch* batch, int32_t dtype,
                const orloj_vectors* k, const orloj_vectors* v, bool write) {
     if (!w) return ORLOJ_E_INVALID;
-    CacheArgs c;
-    Vectors kv, vv;
-    if (int rc = cache_args(w, cache, batch, &c)) return rc;
-    if (int rc = vectors(w, k, c.rows, "k", &kv)) return rc;
-    if (int rc = vectors(w, v, c.rows, "v", &vv)) return rc;
+    CopyArgs a;
+    const CacheArgs& c = a.c;
+    if (int rc = cache_args(w, cache, batch, &a.c)) return rc;
+    if (int rc = vectors(w, k, c.rows, "k", &a.k)) return rc;
+    if (int rc = vectors(w, v, c.rows, "v", &a.v)) return rc;
     if (dtype != ORLOJ_F32 && dtype != ORLOJ_F16 && dtype != ORLOJ_BF16)
         return orloj_ctx_fail(w->ctx, ORLOJ_E_INVALID, "unknown dtype %d", dtype);
     const int64_t groups = (c.rows * 2 * c.heads + kThreads / 16 - 1) / (kThreads / 16);
@@ -828,11 +1244,11 @@ int cache_copy(orloj_worker* w, const orloj_cache* cache, const orloj_batch* bat
     if (write) {
         auto kernel = dtype == ORLOJ_F32 ? cache_write_kernel<F32> : dtype == ORLOJ_F16 ? cache_write_kernel<F16>
                                                                                    : cache_write_kernel<BF16>;
-        return launch(w, "cache_write_kernel", kernel, g, kThreads, c, kv, vv);
+        return launch(w, "cache_write_kernel", kernel, g, kThreads, a);
     }
     auto kernel = dtype == ORLOJ_F32 ? cache_read_kernel<F32> : dtype == ORLOJ_F16 ? cache_read_kernel<F16>
                                                                                : cache_read_kernel<BF16>;
-    return launch(w, "cache_read_kernel", kernel, g, kThreads, c, kv, vv);
+    return launch(w, "cache_read_kernel", kernel, g, kThreads, a);
 }
 
 // Whether 8 elements of 16 bits can be moved as one: every vector starts on 16 bytes.
@@ -965,15 +1381,9 @@ int orloj_worker_adapt(orloj_worker* w, const orloj_adapters* ad, int64_t n_rows
         return orloj_ctx_fail(x, ORLOJ_E_INVALID, "d_base is d_y with another stride");
     if (int rc = enter(w)) return rc;
     if (!n_rows) return ORLOJ_OK;
-    void* h;
-    if (int rc = scratch(w, (size_t)n_rows * ad->rank * sizeof(float), &h)) return rc;
-    const AdaptArgs a{ad->n_adapters, ad->rank, ad->d_in, ad->d_out, n_rows, x_stride, base_stride, y_stride,
-                      ad->d_down, ad->d_up, d_x, d_base, d_y, ad->d_scale, ad->d_rank, d_adapter, (float*)h, w->d_err};
-    const bool half = ad->dtype == ORLOJ_F16;
-    const dim3 gd((unsigned)n_rows), gu((unsigned)n_rows, (ad->d_out + kThreads - 1) / kThreads);
-    if (int rc = launch(w, "adapt_down_kernel", half ? adapt_down_kernel<F16> : adapt_down_kernel<BF16>, gd, kThreads, a))
-        return rc;
-    return launch(w, "adapt_up_kernel", half ? adapt_up_kernel<F16> : adapt_up_kernel<BF16>, gu, kThreads, a);
+    AdaptArgs a{ad->n_adapters, ad->rank, ad->d_in, ad->d_out, n_rows, x_stride, base_stride, y_stride, ad->d_down,
+                ad->d_up, d_x, d_base, d_y, ad->d_scale, ad->d_rank, d_adapter, nullptr, 0, 0, 0, w->d_err};
+    return ad->dtype == ORLOJ_F16 ? adapt<F16>(w, a) : adapt<BF16>(w, a);
 }
 
 int orloj_worker_cache_write(orloj_worker* w, const orloj_cache* cache, const orloj_batch* batch, int32_t dtype,
