@@ -5,7 +5,8 @@
 //   adapt_down_kernel, adapt_up_kernel   h = A_a x, then y = base + s B_a h (and forms
 //                                        for few rows and narrow inputs)
 //   cache_write_kernel, cache_read_kernel  keys and values <-> 8-bit pages
-//   attend_kernel, attend_join_kernel    attention of the rows over the pages
+//   attend_kernel, attend_rows_kernel,   attention of the rows over the pages: few (row,
+//   attend_join_kernel                   head) pairs a request, many, and their splits
 
 #include <hip/hip_fp8.h>
 #include <hip/hip_runtime.h>
@@ -651,7 +652,6 @@ struct AttendArgs {
     float scale;
     int q_heads, group;
     int half;               // q and out are float16, else bfloat16
-    int q_wide, out_wide;   // vectors of 8 elements can be loaded / stored whole
     int block_pairs;        // (row, head) pairs a workgroup takes
     int chunk;              // tokens a workgroup takes, a multiple of 128
     float* part_o;          // [splits][n_rows * q_heads][pad] sums, where a request is split
@@ -689,14 +689,14 @@ __device__ __forceinline__ float column_sum(float x) {
 }
 
 // Eight outputs of a vector, from dimension d on, times inv, rounded once.
-__device__ __forceinline__ void store8(const AttendArgs& a, int64_t at, int d, const float* z, float inv) {
+__device__ __forceinline__ void store8(const AttendArgs& a, int64_t at, int d, const float (&z)[8], float inv) {
     uint16_t* dst = (uint16_t*)a.out.d + at + d;
     ushort8_t h;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         h[j] = a.half ? __builtin_bit_cast(uint16_t, (_Float16)(z[j] * inv)) : __builtin_bit_cast(uint16_t, (__bf16)(z[j] * inv));
-    if (a.out_wide) {
-        if (d < a.c.dim) *(ushort8_t*)dst = h;
+    if (d + 8 <= a.c.dim) {
+        *(ushort8_u*)dst = h;
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -712,6 +712,221 @@ __device__ __forceinline__ int block_last_row(const AttendArgs& a, int i, int j,
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
+// A wave's 16 NT (row, head) pairs, 16 to a column t: queries, what each sees, and the
+// running sums.  Everything in base 2, relative to a reference of the row:
+//   s = q . k scale log2 e,  p = 2^(s + ref),  l = sum p,  o = sum p v,
+// so that out = o / l and lse = (log2 l - ref) / log2 e whatever ref was; ref moves down
+// when scores or value scales outgrow it, and o and l are rescaled then.
+template <int DP, int NT>
+struct Pairs {
+    Half8 q[NT][DP / 32];       // 16-bit floats relative to a power of two of their row
+    float f[NT];                // and what their products are times, >= 0
+    int lim[NT];                // tokens up to it are seen
+    uint64_t mask[NT];          // drafted tokens that are seen
+    float4_t o[NT][DP / 16];
+    float l[NT], ref[NT], top[NT], vlim[NT];
+};
+
+// The request, and the part of its tokens, that a workgroup of `pairs` pairs works on.
+struct Part {
+    int64_t first;              // the request's first row
+    int rows, length, context, pairs;
+    int pair0;                  // the workgroup's first pair
+    int end;                    // tokens any of its rows may see
+    int plain;                  // tokens all of them see
+    int begin, stop;            // its split's
+};
+
+__device__ __forceinline__ bool part_of(const AttendArgs& a, int r, int block, int split, Part& w) {
+    if (!request_of(a.c, r, w.first, w.rows, w.length)) return false;
+    w.pair0 = block * a.block_pairs;
+    w.pairs = w.rows * a.group;
+    if (w.pair0 >= w.pairs) return false;
+    w.context = w.length - w.rows;
+    const int last = (min(w.pair0 + a.block_pairs, w.pairs) - 1) / a.group;
+    w.end = a.tree ? w.length : w.context + last + 1;
+    w.plain = a.tree ? w.context : w.context + w.pair0 / a.group + 1;
+    w.begin = split * a.chunk;
+    w.stop = min(w.begin + a.chunk, w.end);
+    if (a.c.pages == 0) {
+        atomicOr(a.c.err, kErrPage);
+        w.stop = w.begin;
+    }
+    return w.begin < w.end;
+}
+
+template <int DP, int NT>
+__device__ __forceinline__ void start(const AttendArgs& a, const Part& w, int head, int pair_from, Pairs<DP, NT>& x) {
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const float scale = fmaxf(fabsf(a.scale) * kLog2e, 1e-37f);   // 0: equal weights
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int pair = pair_from + 16 * t + n, i = pair / a.group;
+        const bool live = pair < w.pairs;
+        float v[DP / 4], amax = 0.0f;
+        bool bad = false;
+#pragma unroll
+        for (int e = 0; e < DP / 4; e += 8) {
+            const int d = g * (DP / 4) + e;
+            ushort8_t h = {};
+            if (live) {
+                const uint16_t* src = (const uint16_t*)a.q.d + (w.first + i) * a.q.row + (int64_t)(head * a.group + pair - i * a.group) * a.q.head;
+                if (d + 8 <= a.c.dim) {
+                    h = *(const ushort8_u*)(src + d);
+                } else if (d < a.c.dim) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (d + j < a.c.dim) h[j] = src[d + j];
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint16_t u = h[j];
+                v[e + j] = a.half ? (float)__builtin_bit_cast(_Float16, u) : __uint_as_float((uint32_t)u << 16);
+                amax = fmaxf(amax, fabsf(v[e + j]));
+                bad |= !(fabsf(v[e + j]) < INFINITY);
+            }
+        }
+        amax = column_max(bad ? INFINITY : amax);
+        bad = !(amax < INFINITY);
+        const int ex = bad || amax == 0.0f ? 0 : __builtin_amdgcn_frexp_expf(amax);
+        x.f[t] = bad ? NAN : ldexpf(scale, ex);
+        const float sign = a.scale < 0.0f ? -1.0f : 1.0f;
+#pragma unroll
+        for (int e = 0; e < DP / 4; ++e) x.q[t][e / 8].v[e % 8] = (_Float16)(bad ? 0.0f : sign * ldexpf(v[e], -ex));
+        x.lim[t] = live ? (a.tree ? w.context - 1 : w.context + i) : -1;
+        x.mask[t] = live && a.tree ? a.tree[w.first + i] : 0;
+        x.l[t] = 0.0f;
+        // nothing seen: a reference that any score moves
+        x.top[t] = -3e38f;      // largest score so far (of the four lanes of a column)
+        x.vlim[t] = 0x1p-88f;   // largest value scale its reference allows
+        x.ref[t] = 3e38f;
+#pragma unroll
+        for (int j = 0; j < DP / 16; ++j) x.o[t][j] = float4_t{0, 0, 0, 0};
+    }
+}
+
+// Products of column t with 32 tokens from t0 on -> their weights times the value
+// scales, as the operand of the product with V.  all: every row sees all of them.
+template <int DP, int NT>
+__device__ __forceinline__ half8_t weigh(const Part& w, Pairs<DP, NT>& x, int t, const float4_t (&s)[2], const float4_t (&ks)[2],
+                                         const float4_t (&vs)[2], int t0, bool all) {
+    const int g = threadIdx.x >> 4 & 3;
+    float u[8], v[8], mx = -INFINITY, vmax = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        u[j] = s[j >> 2][j & 3] * ks[j >> 2][j & 3];
+        v[j] = vs[j >> 2][j & 3];
+    }
+    if (!all) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int tok = t0 + 16 * (j >> 2) + 4 * g + (j & 3);
+            const int drafted = (int)(x.mask[t] >> ((tok - w.context) & 63)) & 1;
+            const bool sees = (tok < w.stop) & ((tok <= x.lim[t]) | drafted);
+            u[j] = sees ? u[j] : -INFINITY;
+            v[j] = sees ? v[j] : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        mx = fmaxf(mx, u[j]);
+        vmax = fmaxf(vmax, v[j]);
+    }
+    // scores up to 2^6 above the reference's, value scales up to 4 above its, so that
+    // weights of up to 2^14 fit a 16-bit float and all but those 2^-20 below the largest
+    // keep its 11 bits
+    mx *= x.f[t];
+    if (__any(mx > x.top[t] + 6.0f || vmax > x.vlim[t])) {
+        x.top[t] = fmaxf(x.top[t], column_max(mx));
+        const float most = column_max(vmax);
+        if (most > x.vlim[t]) x.vlim[t] = ldexpf(1.0f, min(__builtin_amdgcn_frexp_expf(most), 100) + 2);
+        const float now = 8.0f - __builtin_amdgcn_logf(x.vlim[t]) - x.top[t];
+        const float by = __builtin_amdgcn_exp2f(now - x.ref[t]);
+        x.ref[t] = now;
+        x.l[t] *= by;
+#pragma unroll
+        for (int j = 0; j < DP / 16; ++j) x.o[t][j] *= by;
+    }
+    half8_t p;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(u[j], x.f[t], x.ref[t]));
+        x.l[t] += e;
+        p[j] = (_Float16)(e * v[j]);
+    }
+    return p;
+}
+
+// Eight codes of a K row (two words) as the product's operand.
+template <int FMT>
+__device__ __forceinline__ half8_t k_operand(uint32_t a, uint32_t b) {
+    if (FMT == ORLOJ_CACHE_INT8) {
+        a ^= 0x80808080u;
+        b ^= 0x80808080u;
+    }
+    Half8 k;
+    k.p[0] = two_codes<FMT, false>(a);
+    k.p[1] = two_codes<FMT, true>(a);
+    k.p[2] = two_codes<FMT, false>(b);
+    k.p[3] = two_codes<FMT, true>(b);
+    return k.v;
+}
+
+// Four dimensions (a word each) of eight tokens -> per dimension, the eight tokens as the
+// product's operand.
+template <int FMT>
+__device__ __forceinline__ void v_operands(const uint32_t (&w)[8], half8_t (&v)[4]) {
+    uint32_t lo[4], hi[4];   // bytes 0, 1 and 2, 3 of two tokens each
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t a = w[2 * i], b = w[2 * i + 1];
+        if (FMT == ORLOJ_CACHE_INT8) {
+            a ^= 0x80808080u;
+            b ^= 0x80808080u;
+        }
+        lo[i] = __builtin_amdgcn_perm(b, a, 0x05010400u);
+        hi[i] = __builtin_amdgcn_perm(b, a, 0x07030602u);
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        Half8 x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.p[i] = b & 1 ? two_codes<FMT, true>(b < 2 ? lo[i] : hi[i]) : two_codes<FMT, false>(b < 2 ? lo[i] : hi[i]);
+        v[b] = x.v;
+    }
+}
+
+// The page of a request's 16-token part, 0 where the table is wrong.
+__device__ __forceinline__ int page_of_part(const CacheArgs& c, int r, int part) {
+    const int p = c.table[(int64_t)r * c.max_pages + (part >> (c.shift - 4))];
+    if (p >= 0 && p < c.pages) return p;
+    atomicOr(c.err, kErrPage);
+    return 0;
+}
+// Where the part starts among all (page, head, slot) triples.
+__device__ __forceinline__ int64_t part_slot(const CacheArgs& c, int page, int head, int part) {
+    return (((int64_t)page * c.heads + head) << c.shift) + ((part << 4) & (c.page - 1));
+}
+
+// Eight dimensions of a pair's output, and its lse with the first: final, or a split's
+// sums for attend_join_kernel.
+template <int DP>
+__device__ __forceinline__ void put_out(const AttendArgs& a, const Part& w, int split, int head, int pair, int d, const float (&z)[8],
+                                        float sum, float ref) {
+    const int i = pair / a.group, qh = head * a.group + pair - i * a.group;
+    const int64_t global = (w.first + i) * a.q_heads + qh;
+    if (a.chunk >= w.end) {
+        store8(a, (w.first + i) * a.out.row + (int64_t)qh * a.out.head, d, z, sum == 0.0f ? 0.0f : 1.0f / sum);
+        if (d == 0 && a.lse) a.lse[global] = sum == 0.0f ? -INFINITY : (__builtin_amdgcn_logf(sum) - ref) * kLn2;
+    } else {
+        const int64_t at = (int64_t)split * a.c.rows * a.q_heads + global;
+        *(float4_t*)(a.part_o + at * DP + d) = float4_t{z[0], z[1], z[2], z[3]};
+        *(float4_t*)(a.part_o + at * DP + d + 4) = float4_t{z[4], z[5], z[6], z[7]};
+        if (d == 0) a.part_cl[at] = float2{ref, sum};
+    }
+}
+
 // One tile of 32 tokens as a lane loads it: two 16-token parts of a page.
 template <int DP>
 struct Tile {
@@ -720,12 +935,9 @@ struct Tile {
     float4_t ks[2], vs[2];        // scales of those eight tokens
 };
 
-// out = softmax(scale q K^T) V for 16 NT (row, head) pairs that share a key head,
-// over a.chunk tokens.  Everything in base 2, relative to a reference c of the row:
-//   s = q . k scale log2 e,  p = 2^(s + c),  l = sum p,  o = sum p v,
-// so that out = o / l and lse = (log2 l - c) / log2 e whatever c was; c moves down
-// when scores or value scales outgrow it, and o and l are rescaled then.
-//   S^T = K Q^T   v_mfma_f32_16x16x32_f16, a tile's tokens by 16 rows
+// out = softmax(scale q K^T) V for few pairs that share a key head (16 NT), over a.chunk
+// tokens:
+//   S^T = K Q^T   v_mfma_f32_16x16x32_f16, a tile's tokens by 16 pairs
 //   O^T = V^T P^T the same; S^T's registers hold what P^T's operand needs
 // The order of the k index is free as long as both operands agree, so no operand
 // goes through LDS: a lane loads its share of the page rows whole (16 bytes of K,
@@ -733,7 +945,7 @@ struct Tile {
 // Four waves take every fourth tile, the next one's loads in flight; their sums meet
 // in LDS.
 template <int FMT, int DP, int NT>
-__global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend_kernel(AttendArgs a) {
     constexpr int R = 16 * NT, ND = DP / 64, MT = DP / 16;
     __shared__ __attribute__((aligned(16))) float o_sum[R][DP + 4];
     __shared__ float c_of[kWaves][R], l_of[kWaves][R];
@@ -741,113 +953,30 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int split = blockIdx.x, head = blockIdx.y % c.heads, block = blockIdx.y / c.heads, r = blockIdx.z;
+    Part w;
+    if (!part_of(a, r, block, split, w)) return;
+    Pairs<DP, NT> q;
+    start<DP, NT>(a, w, head, w.pair0, q);
 
-    int64_t first;
-    int rows, length;
-    if (!request_of(c, r, first, rows, length)) return;
-    const int pair0 = block * R, pairs = rows * a.group;
-    if (pair0 >= pairs) return;
-    const int context = length - rows;
-    const int i_first = pair0 / a.group, i_last = (min(pair0 + R, pairs) - 1) / a.group;
-    const int end = a.tree ? length : context + i_last + 1;   // tokens any row may see
-    const int plain = a.tree ? context : context + i_first + 1; // tokens every row sees
-    const int begin = split * a.chunk, stop = min(begin + a.chunk, end);
-    if (begin >= stop && split > 0) return;
+    const int tiles = (w.stop - w.begin + 31) >> 5;
+    const int last_part = (w.end - 1) >> 4;   // 16-token parts beyond it hold nothing
+    int page_of = 0;                          // lane 2 i + part: the page of the wave's i-th tile from the last load
 
-    // queries: 16-bit floats relative to a power of two of their row
-    Half8 q[NT][DP / 32];
-    float f[NT];
-    int lim[NT];
-    uint64_t mask[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int pair = pair0 + 16 * t + n;
-        const int i = pair / a.group;
-        const bool live = pair < pairs;
-        const int64_t at = (first + i) * a.q.row + (int64_t)(head * a.group + pair - i * a.group) * a.q.head;
-        float x[DP / 4], amax = 0.0f;
-#pragma unroll
-        for (int e = 0; e < DP / 4; ++e) x[e] = 0.0f;
-        if (live) {
-            const uint16_t* src = (const uint16_t*)a.q.d + at;
-#pragma unroll
-            for (int e = 0; e < DP / 4; e += 8) {
-                const int d = g * (DP / 4) + e;
-                ushort8_t h = {};
-                if (a.q_wide) {
-                    if (d < c.dim) h = *(const ushort8_t*)(src + d);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (d + j < c.dim) h[j] = src[d + j];
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint16_t u = h[j];
-                    x[e + j] = a.half ? (float)__builtin_bit_cast(_Float16, u) : __builtin_bit_cast(float, (uint32_t)u << 16);
-                }
-            }
-        }
-        bool bad = false;
-#pragma unroll
-        for (int e = 0; e < DP / 4; ++e) {
-            amax = fmaxf(amax, fabsf(x[e]));
-            bad |= !(fabsf(x[e]) < INFINITY);
-        }
-        amax = column_max(bad ? INFINITY : amax);
-        bad = !(amax < INFINITY);
-        const int ex = bad || amax == 0.0f ? 0 : __builtin_amdgcn_frexp_expf(amax);
-        f[t] = bad ? NAN : ldexpf(a.scale * kLog2e, ex);
-#pragma unroll
-        for (int e = 0; e < DP / 4; ++e)
-            q[t][e / 8].v[e % 8] = (_Float16)(bad ? 0.0f : ldexpf(x[e], -ex));
-        lim[t] = live ? (a.tree ? context - 1 : context + i) : -1;
-        mask[t] = live && a.tree ? a.tree[first + i] : 0;
-    }
-
-    float4_t o[NT][MT];
-    float l[NT], ref[NT], top[NT], vlim[NT];
-    // nothing seen: a reference that any score moves
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        l[t] = 0.0f;
-        top[t] = -3e38f;      // largest score so far (of the four lanes of a column)
-        vlim[t] = 0x1p-88f;   // largest value scale its reference allows
-        ref[t] = 3e38f;
-#pragma unroll
-        for (int j = 0; j < MT; ++j) o[t][j] = float4_t{0, 0, 0, 0};
-    }
-
-    const int tiles = stop > begin ? (stop - begin + 31) >> 5 : 0;
-    const int last_part = (end - 1) >> 4;   // 16-token parts beyond it hold nothing
-    const int32_t* table = c.table + (int64_t)r * c.max_pages;
-    int page_of = 0;                        // lane 2 i + part: the page of the wave's i-th tile from the last load
-
-    auto load_pages = [&](int it) {
-        const int tile = wave + (it + (lane >> 1)) * kWaves;
-        const int part = min((begin >> 4) + 2 * tile + (lane & 1), last_part);
-        int p = table[part >> (c.shift - 4)];
-        if (p < 0 || p >= c.pages) {
-            atomicOr(c.err, kErrPage);
-            p = 0;
-        }
-        page_of = p;
-    };
     auto load = [&](int it, Tile<DP>& x) {
-        if ((it & 31) == 0) load_pages(it);
-        const int t0 = begin + (wave + it * kWaves) * 32;
+        if ((it & 31) == 0)
+            page_of = page_of_part(c, r, min((w.begin >> 4) + 2 * (wave + (it + (lane >> 1)) * kWaves) + (lane & 1), last_part));
+        const int t0 = w.begin + (wave + it * kWaves) * 32;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int part = min((t0 >> 4) + h, last_part);
-            const int p = __builtin_amdgcn_readlane(page_of, (2 * it + h) & 63);
-            const int64_t slot = (((int64_t)p * c.heads + head) << c.shift) + ((part << 4) & (c.page - 1));
+            const int64_t slot = part_slot(c, __builtin_amdgcn_readlane(page_of, (2 * it + h) & 63), head, part);
             const uint8_t* kp = c.k + slot * DP;
             const uint8_t* vp = c.v + slot * DP;
 #pragma unroll
             for (int j = 0; j < ND; ++j) x.k[h][j] = *(const uint4_t*)(kp + n * DP + g * (DP / 4) + 16 * j);
             // tokens past the end may hold codes that no weight of zero removes (NaN): the
             // last token instead
-            const int most = min(15, end - 1 - (part << 4));
+            const int most = min(15, w.end - 1 - (part << 4));
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint8_t* row = vp + min(4 * g + i, most) * DP + n * (DP / 16);
@@ -859,7 +988,7 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
         }
     };
     auto use = [&](int it, Tile<DP>& x) {
-        const int t0 = begin + (wave + it * kWaves) * 32;
+        const int t0 = w.begin + (wave + it * kWaves) * 32;
         float4_t s[NT][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -867,104 +996,32 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
             for (int t = 0; t < NT; ++t) s[t][h] = float4_t{0, 0, 0, 0};
 #pragma unroll
             for (int e = 0; e < DP / 32; ++e) {
-                Half8 k;
+                const half8_t k = k_operand<FMT>(x.k[h][e / 2][(e & 1) * 2], x.k[h][e / 2][(e & 1) * 2 + 1]);
 #pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    uint32_t u = x.k[h][e / 2][(e & 1) * 2 + w];
-                    if (FMT == ORLOJ_CACHE_INT8) u ^= 0x80808080u;
-                    k.p[2 * w] = two_codes<FMT, false>(u);
-                    k.p[2 * w + 1] = two_codes<FMT, true>(u);
-                }
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-                    s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k.v, q[t][e].v, s[t][h], 0, 0, 0);
+                for (int t = 0; t < NT; ++t) s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q.q[t][e].v, s[t][h], 0, 0, 0);
             }
         }
-        const bool all = t0 + 32 <= plain && t0 + 32 <= stop;
-        Half8 p[NT];
-        float big = 0.0f;
+        const bool all = t0 + 32 <= min(w.plain, w.stop);
+        half8_t p[NT];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) big = fmaxf(big, x.vs[h][i]);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            float vs[8], w[8];
-            float mx = -INFINITY, vmax = big;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                w[j] = s[t][j >> 2][j & 3] * x.ks[j >> 2][j & 3] * f[t];
-                vs[j] = x.vs[j >> 2][j & 3];
-            }
-            if (!all) {
-                vmax = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int tok = t0 + 16 * (j >> 2) + 4 * g + (j & 3);
-                    const int drafted = (int)(mask[t] >> ((tok - context) & 63)) & 1;
-                    const bool sees = (tok < stop) & ((tok <= lim[t]) | drafted);
-                    w[j] = sees ? w[j] : -INFINITY;
-                    vs[j] = sees ? vs[j] : 0.0f;
-                    vmax = fmaxf(vmax, vs[j]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) mx = fmaxf(mx, w[j]);
-            // scores up to 2^6 above the reference's, value scales up to 4 above its, so
-            // that weights of up to 2^14 fit a 16-bit float and all but those 2^-20 below
-            // the largest keep its 11 bits
-            if (__any(mx > top[t] + 6.0f || vmax > vlim[t])) {
-                top[t] = fmaxf(top[t], column_max(mx));
-                const float most = column_max(vmax);
-                if (most > vlim[t]) vlim[t] = ldexpf(1.0f, min(__builtin_amdgcn_frexp_expf(most), 100) + 2);
-                const float now = 8.0f - __builtin_amdgcn_logf(vlim[t]) - top[t];
-                const float by = __builtin_amdgcn_exp2f(now - ref[t]);
-                ref[t] = now;
-                l[t] *= by;
-#pragma unroll
-                for (int j = 0; j < MT; ++j) o[t][j] *= by;
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                w[j] = __builtin_amdgcn_exp2f(w[j] + ref[t]);
-                l[t] += w[j];
-                w[j] *= vs[j];
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p[t].v[j] = (_Float16)w[j];
-        }
+        for (int t = 0; t < NT; ++t) p[t] = weigh<DP, NT>(w, q, t, s[t], x.ks, x.vs, t0, all);
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
-            uint32_t lo[4], hi[4];   // bytes 0, 1 and 2, 3 of two tokens each
+            uint32_t words[8];
+            half8_t v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t u = x.v[2 * i][d], w = x.v[2 * i + 1][d];
-                if (FMT == ORLOJ_CACHE_INT8) {
-                    u ^= 0x80808080u;
-                    w ^= 0x80808080u;
-                }
-                lo[i] = __builtin_amdgcn_perm(w, u, 0x05010400u);
-                hi[i] = __builtin_amdgcn_perm(w, u, 0x07030602u);
-            }
+            for (int i = 0; i < 8; ++i) words[i] = x.v[i][d];
+            v_operands<FMT>(words, v);
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                Half8 v;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t u = b < 2 ? lo[i] : hi[i];
-                    v.p[i] = b & 1 ? two_codes<FMT, true>(u) : two_codes<FMT, false>(u);
-                }
+            for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
-                    o[t][4 * d + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v.v, p[t].v, o[t][4 * d + b], 0, 0, 0);
-            }
+                    q.o[t][4 * d + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[b], p[t], q.o[t][4 * d + b], 0, 0, 0);
         }
     };
 
     const int mine = tiles > wave ? (tiles - wave + kWaves - 1) / kWaves : 0;
-    if (c.pages == 0) {
-        atomicOr(c.err, kErrPage);
-    } else if (mine > 0) {
+    if (mine > 0) {
         Tile<DP> x, y;
         load(0, x);
         int it = 0;
@@ -980,10 +1037,10 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
     // the four waves' sums, in turn, so that the order of the additions is fixed
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        l[t] = column_sum(l[t]);
+        q.l[t] = column_sum(q.l[t]);
         if (g == 0) {
-            c_of[wave][16 * t + n] = ref[t];
-            l_of[wave][16 * t + n] = l[t];
+            c_of[wave][16 * t + n] = q.ref[t];
+            l_of[wave][16 * t + n] = q.l[t];
         }
     }
     __syncthreads();
@@ -991,10 +1048,10 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int k = 16 * t + n;
-        by[t] = __builtin_amdgcn_exp2f(fminf(fminf(c_of[0][k], c_of[1][k]), fminf(c_of[2][k], c_of[3][k])) - ref[t]);
+        by[t] = __builtin_amdgcn_exp2f(fminf(fminf(c_of[0][k], c_of[1][k]), fminf(c_of[2][k], c_of[3][k])) - q.ref[t]);
     }
-    for (int w = 0; w < kWaves; ++w) {
-        if (w == wave) {
+    for (int v = 0; v < kWaves; ++v) {
+        if (v == wave) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -1002,37 +1059,173 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
                     float* at = &o_sum[16 * t + n][(4 * g + i) * MT];
 #pragma unroll
                     for (int j = 0; j < MT; j += 4) {
-                        float4_t x = {o[t][j][i], o[t][j + 1][i], o[t][j + 2][i], o[t][j + 3][i]};
+                        float4_t x = {q.o[t][j][i], q.o[t][j + 1][i], q.o[t][j + 2][i], q.o[t][j + 3][i]};
                         x *= by[t];
-                        *(float4_t*)(at + j) = w ? *(float4_t*)(at + j) + x : x;
+                        *(float4_t*)(at + j) = v ? *(float4_t*)(at + j) + x : x;
                     }
                 }
         }
         __syncthreads();
     }
-
-    const bool whole = a.chunk >= end;
     for (int k = threadIdx.x; k < R * (DP / 8); k += kThreads) {
-        const int row = k / (DP / 8), d = k % (DP / 8) * 8, pair = pair0 + row;
-        if (pair >= pairs) break;
-        const float m = fminf(fminf(c_of[0][row], c_of[1][row]), fminf(c_of[2][row], c_of[3][row]));
-        float sum = 0.0f;
+        const int row = k / (DP / 8), d = k % (DP / 8) * 8;
+        if (w.pair0 + row >= w.pairs) break;
+        const float ref = fminf(fminf(c_of[0][row], c_of[1][row]), fminf(c_of[2][row], c_of[3][row]));
+        float sum = 0.0f, z[8];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) sum += l_of[w][row] * __builtin_amdgcn_exp2f(m - c_of[w][row]);
-        const int i = pair / a.group, qh = head * a.group + pair - i * a.group;
-        const int64_t global = (first + i) * a.q_heads + qh;
-        const float4_t x = *(float4_t*)&o_sum[row][d], y = *(float4_t*)&o_sum[row][d + 4];
-        if (whole) {
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            float z[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-            store8(a, (first + i) * a.out.row + (int64_t)qh * a.out.head, d, z, inv);
-            if (d == 0 && a.lse) a.lse[global] = sum == 0.0f ? -INFINITY : (__builtin_amdgcn_logf(sum) - m) * kLn2;
-        } else {
-            const int64_t at = (int64_t)split * c.rows * a.q_heads + global;
-            *(float4_t*)(a.part_o + at * DP + d) = x;
-            *(float4_t*)(a.part_o + at * DP + d + 4) = y;
-            if (d == 0) a.part_cl[at] = float2{m, sum};
+        for (int v = 0; v < kWaves; ++v) sum += l_of[v][row] * __builtin_amdgcn_exp2f(ref - c_of[v][row]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = o_sum[row][d + j];
+        put_out<DP>(a, w, split, head, w.pair0 + row, d, z, sum, ref);
+    }
+}
+
+// The same for many pairs (trees, chunks of a prompt): 16 NT a wave, their four waves
+// share the tokens.  A tile of TK tokens is read once, becomes 16-bit floats once and goes
+// to LDS in the order of the products' operands (16 bytes a lane, no conflicts), one tile
+// ahead of the products; its codes are in flight one further ahead.
+template <int FMT, int DP, int NT>
+__global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs a) {
+    constexpr int ND = DP / 64, MT = DP / 16, TK = DP <= 128 ? 64 : 32, PARTS = TK / 16;
+    constexpr int KU = PARTS * ND, KW = (KU + 3) / 4;          // 16-byte pieces of K, of them a wave's
+    constexpr int VU = PARTS / 2 * ND, VW = (VU + 3) / 4;      // words of V for 32 tokens, of them a wave's
+    __shared__ half8_t ks_[2][PARTS][2 * ND][64];   // part, step of 32 dimensions
+    __shared__ half8_t vs_[2][PARTS / 2][MT][64];   // 32 tokens, 16 dimensions
+    __shared__ __attribute__((aligned(16))) float scale[2][2][TK];
+    const CacheArgs& c = a.c;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int blocks = gridDim.y / c.heads;
+    // the blocks that see most first
+    const int split = blockIdx.x, head = blockIdx.y % c.heads, block = blocks - 1 - blockIdx.y / c.heads, r = blockIdx.z;
+    Part w;
+    if (!part_of(a, r, block, split, w)) return;
+    Pairs<DP, NT> q;
+    const int pair_from = w.pair0 + 16 * NT * wave;
+    start<DP, NT>(a, w, head, pair_from, q);
+
+    const int tiles = (w.stop - w.begin + TK - 1) / TK;
+    const int last_part = (w.end - 1) >> 4;
+    int page_of = 0;                    // lane i: the page of the i-th part from the last load
+
+    uint4_t kr[KW];
+    uint32_t vr[VW][8];
+    float sr = 0.0f;
+    auto load = [&](int it) {
+        constexpr int TILES = 64 / PARTS;
+        if (it % TILES == 0) page_of = page_of_part(c, r, min((w.begin >> 4) + it * PARTS + lane, last_part));
+        const int in = it % TILES * PARTS, part0 = (w.begin >> 4) + it * PARTS;
+#pragma unroll
+        for (int i = 0; i < KW; ++i) {
+            const int u = wave + 4 * i, h = u / ND;
+            if (KU % 4 && u >= KU) break;
+            const int64_t slot = part_slot(c, __builtin_amdgcn_readlane(page_of, in + h), head, min(part0 + h, last_part));
+            kr[i] = *(const uint4_t*)(c.k + (slot + n) * DP + g * (DP / 4) + 16 * (u % ND));
         }
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+            const int u = wave + 4 * i;
+            if (VU % 4 && u >= VU) break;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int p = 2 * (u / ND) + h, part = min(part0 + p, last_part);
+                const int64_t slot = part_slot(c, __builtin_amdgcn_readlane(page_of, in + p), head, part);
+                const int most = min(15, w.end - 1 - (part << 4));      // as in attend_kernel
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    vr[i][4 * h + j] = *(const uint32_t*)(c.v + (slot + min(4 * g + j, most)) * DP + n * (DP / 16) + 4 * (u % ND));
+            }
+        }
+        const int tok = threadIdx.x & (TK - 1);
+        const int page = __shfl(page_of, in + (tok >> 4), 64);
+        if (threadIdx.x < 2 * TK)
+            sr = (threadIdx.x < TK ? c.ks : c.vs)[part_slot(c, page, head, min(part0 + (tok >> 4), last_part)) + (tok & 15)];
+    };
+    auto stage = [&](int b) {
+#pragma unroll
+        for (int i = 0; i < KW; ++i) {
+            const int u = wave + 4 * i;
+            if (KU % 4 && u >= KU) break;
+            ks_[b][u / ND][2 * (u % ND)][lane] = k_operand<FMT>(kr[i][0], kr[i][1]);
+            ks_[b][u / ND][2 * (u % ND) + 1][lane] = k_operand<FMT>(kr[i][2], kr[i][3]);
+        }
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+            const int u = wave + 4 * i;
+            if (VU % 4 && u >= VU) break;
+            half8_t v[4];
+            v_operands<FMT>(vr[i], v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) vs_[b][u / ND][4 * (u % ND) + j][lane] = v[j];
+        }
+        if (threadIdx.x < 2 * TK) scale[b][threadIdx.x / TK][threadIdx.x & (TK - 1)] = sr;
+    };
+
+    // tokens that the wave's rows may see
+    const int wave_last = min(pair_from + 16 * NT, w.pairs) - 1;
+    const int wave_stop = pair_from >= w.pairs ? w.begin : a.tree ? w.stop : min(w.stop, w.context + wave_last / a.group + 1);
+    if (tiles > 0) {
+        load(0);
+        stage(0);
+        if (tiles > 1) load(1);
+        __syncthreads();
+    }
+    for (int it = 0; it < tiles; ++it) {
+        const int b = it & 1, t0 = w.begin + it * TK;
+        if (t0 < wave_stop) {
+            const bool all = t0 + TK <= min(w.plain, w.stop);
+#pragma unroll
+            for (int h = 0; h < PARTS / 2; ++h) {
+                float4_t s[NT][2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) s[t][i] = float4_t{0, 0, 0, 0};
+#pragma unroll
+                    for (int e = 0; e < 2 * ND; ++e) {
+                        const half8_t k = ks_[b][2 * h + i][e][lane];
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+                            s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q.q[t][e].v, s[t][i], 0, 0, 0);
+                    }
+                }
+                float4_t ks[2], vs[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    ks[i] = *(const float4_t*)&scale[b][0][32 * h + 16 * i + 4 * g];
+                    vs[i] = *(const float4_t*)&scale[b][1][32 * h + 16 * i + 4 * g];
+                }
+                half8_t p[NT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) p[t] = weigh<DP, NT>(w, q, t, s[t], ks, vs, t0 + 32 * h, all);
+#pragma unroll
+                for (int j = 0; j < MT; ++j) {
+                    const half8_t v = vs_[b][h][j][lane];
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) q.o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[t], q.o[t][j], 0, 0, 0);
+                }
+            }
+        }
+        if (it + 1 < tiles) stage(b ^ 1);
+        if (it + 2 < tiles) load(it + 2);
+        __syncthreads();
+    }
+
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const float sum = column_sum(q.l[t]);
+        const int pair = pair_from + 16 * t + n;
+        if (pair >= w.pairs) continue;
+        // the lane's dimensions are (4 g + i) MT + j, so two i hold MT / 4 runs of eight
+#pragma unroll
+        for (int i = 0; i < 4; i += 2)
+#pragma unroll
+            for (int m = 0; m < 2 * MT; m += 8) {
+                float z[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) z[k] = q.o[t][(m + k) % MT][i + (m + k) / MT];
+                put_out<DP>(a, w, split, head, pair, (4 * g + i) * MT + m, z, sum, q.ref[t]);
+            }
     }
 }
 
@@ -1251,22 +1444,18 @@ int cache_copy(orloj_worker* w, const orloj_cache* cache, const orloj_batch* bat
     return launch(w, "cache_read_kernel", kernel, g, kThreads, a);
 }
 
-// Whether 8 elements of 16 bits can be moved as one: every vector starts on 16 bytes.
-bool wide(const Vectors& v, int dim) {
-    return ((uintptr_t)v.d & 15) == 0 && v.row % 8 == 0 && v.head % 8 == 0 && dim % 8 == 0;
-}
-
-template <int FMT, int DP, int NT>
-int attend_tiles(orloj_worker* w, AttendArgs& a) {
-    const int64_t pairs = (int64_t)a.c.max_rows * a.group, blocks = (pairs + 16 * NT - 1) / (16 * NT);
-    a.block_pairs = 16 * NT;
+// Launches `kernel` over blocks of block_pairs pairs, split over tokens where there are
+// few of them, and the join of the splits.
+template <int DP>
+int attend_blocks(orloj_worker* w, AttendArgs& a, const char* what, void (*kernel)(AttendArgs), int block_pairs, int per_unit) {
+    const int64_t pairs = (int64_t)a.c.max_rows * a.group, blocks = (pairs + block_pairs - 1) / block_pairs;
+    a.block_pairs = block_pairs;
     const int64_t groups = (int64_t)a.c.requests * a.c.heads * blocks;
-    // Eight workgroups a unit where there are fewer, from at least 256 tokens each
-    const int64_t want = (8 * (int64_t)w->ctx->n_cu + groups - 1) / groups;
+    // per_unit workgroups a unit where there are fewer, from at least 256 tokens each
+    const int64_t want = (per_unit * (int64_t)w->ctx->n_cu + groups - 1) / groups;
     const int64_t most = std::max<int64_t>(1, (a.c.max_length + 255) / 256);
-    const int64_t splits0 = std::min(want, most);
-    a.chunk = (int)(((a.c.max_length + splits0 - 1) / splits0 + 127) / 128 * 128);
-    a.chunk = std::max(a.chunk, 128);
+    const int64_t parts = std::min(want, most);
+    a.chunk = std::max(128, (int)(((a.c.max_length + parts - 1) / parts + 127) / 128 * 128));
     const int splits = std::max(1, (a.c.max_length + a.chunk - 1) / a.chunk);
     if (blocks * a.c.heads > 65535)
         return orloj_ctx_fail(w->ctx, ORLOJ_E_UNSUPPORTED, "%lld (row, head) pairs of one request are too many",
@@ -1278,27 +1467,30 @@ int attend_tiles(orloj_worker* w, AttendArgs& a) {
         a.part_o = (float*)p;
         a.part_cl = (float2*)(a.part_o + n * DP);
     }
-    const dim3 grid(splits, (unsigned)(blocks * a.c.heads), a.c.requests);
-    if (int rc = launch(w, "attend_kernel", attend_kernel<FMT, DP, NT>, grid, kThreads, a)) return rc;
+    if (int rc = launch(w, what, kernel, dim3(splits, (unsigned)(blocks * a.c.heads), a.c.requests), kThreads, a)) return rc;
     if (splits == 1) return ORLOJ_OK;
     return launch(w, "attend_join_kernel", attend_join_kernel<DP>, dim3(a.c.max_rows, a.q_heads, a.c.requests), kThreads, a);
 }
 
+template <int FMT, int DP>
+int attend_dim(orloj_worker* w, AttendArgs& a) {
+    const int64_t pairs = (int64_t)a.c.max_rows * a.group;
+    if (pairs <= 16) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, DP, 1>, 16, 4);
+    // beyond 128 dimensions the registers hold the sums of 16 pairs a wave
+    if constexpr (DP <= 128) {
+        if (pairs <= 32) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, DP, 2>, 32, 4);
+        if (pairs > 64) return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, DP, 2>, 128, 4);
+    }
+    return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, DP, 1>, 64, 4);
+}
+
 template <int FMT>
 int attend(orloj_worker* w, AttendArgs& a) {
-    const int64_t pairs = (int64_t)a.c.max_rows * a.group;
-    const int tiles = pairs <= 16 ? 1 : pairs <= 32 || a.c.pad > 128 ? 2 : 4;
-    switch (a.c.pad / 64 * 8 + tiles) {
-        case 9: return attend_tiles<FMT, 64, 1>(w, a);
-        case 10: return attend_tiles<FMT, 64, 2>(w, a);
-        case 12: return attend_tiles<FMT, 64, 4>(w, a);
-        case 17: return attend_tiles<FMT, 128, 1>(w, a);
-        case 18: return attend_tiles<FMT, 128, 2>(w, a);
-        case 20: return attend_tiles<FMT, 128, 4>(w, a);
-        case 25: return attend_tiles<FMT, 192, 1>(w, a);
-        case 26: return attend_tiles<FMT, 192, 2>(w, a);
-        case 33: return attend_tiles<FMT, 256, 1>(w, a);
-        default: return attend_tiles<FMT, 256, 2>(w, a);
+    switch (a.c.pad) {
+        case 64: return attend_dim<FMT, 64>(w, a);
+        case 128: return attend_dim<FMT, 128>(w, a);
+        case 192: return attend_dim<FMT, 192>(w, a);
+        default: return attend_dim<FMT, 256>(w, a);
     }
 }
 
@@ -1423,8 +1615,6 @@ int orloj_worker_attend(orloj_worker* w, const orloj_cache* cache, const orloj_b
     a.q_heads = n_q_heads;
     a.group = n_q_heads / a.c.heads;
     a.half = dtype == ORLOJ_F16;
-    a.q_wide = wide(a.q, a.c.dim);
-    a.out_wide = wide(a.out, a.c.dim);
     return a.c.format == ORLOJ_CACHE_INT8 ? attend<ORLOJ_CACHE_INT8>(w, a) : attend<ORLOJ_CACHE_FP8>(w, a);
 }
 
