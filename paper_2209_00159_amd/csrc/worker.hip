@@ -973,18 +973,18 @@ __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend
             const uint8_t* kp = c.k + slot * DP;
             const uint8_t* vp = c.v + slot * DP;
 #pragma unroll
-            for (int j = 0; j < ND; ++j) x.k[h][j] = *(const uint4_t*)(kp + n * DP + g * (DP / 4) + 16 * j);
+            for (int j = 0; j < ND; ++j) x.k[h][j] = *(const uint4_t*)(kp + 16 * j + (uint32_t)(n * DP + g * (DP / 4)));
             // tokens past the end may hold codes that no weight of zero removes (NaN): the
             // last token instead
             const int most = min(15, w.end - 1 - (part << 4));
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint8_t* row = vp + min(4 * g + i, most) * DP + n * (DP / 16);
+                const uint8_t* row = vp + (uint32_t)(min(4 * g + i, most) * DP + n * (DP / 16));
 #pragma unroll
                 for (int j = 0; j < ND; ++j) x.v[4 * h + i][j] = ((const uint32_t*)row)[j];
             }
-            x.ks[h] = *(const float4_t*)(c.ks + slot + 4 * g);
-            x.vs[h] = *(const float4_t*)(c.vs + slot + 4 * g);
+            x.ks[h] = *(const float4_t*)(c.ks + slot + (uint32_t)(4 * g));
+            x.vs[h] = *(const float4_t*)(c.vs + slot + (uint32_t)(4 * g));
         }
     };
     auto use = [&](int it, Tile<DP>& x) {
@@ -1120,7 +1120,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs a) 
             const int u = wave + 4 * i, h = u / ND;
             if (KU % 4 && u >= KU) break;
             const int64_t slot = part_slot(c, __builtin_amdgcn_readlane(page_of, in + h), head, min(part0 + h, last_part));
-            kr[i] = *(const uint4_t*)(c.k + (slot + n) * DP + g * (DP / 4) + 16 * (u % ND));
+            kr[i] = *(const uint4_t*)(c.k + slot * DP + 16 * (u % ND) + (uint32_t)(n * DP + g * (DP / 4)));
         }
 #pragma unroll
         for (int i = 0; i < VW; ++i) {
@@ -1130,10 +1130,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs a) 
             for (int h = 0; h < 2; ++h) {
                 const int p = 2 * (u / ND) + h, part = min(part0 + p, last_part);
                 const int64_t slot = part_slot(c, __builtin_amdgcn_readlane(page_of, in + p), head, part);
+                const uint8_t* at = c.v + slot * DP + 4 * (u % ND);
                 const int most = min(15, w.end - 1 - (part << 4));      // as in attend_kernel
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    vr[i][4 * h + j] = *(const uint32_t*)(c.v + (slot + min(4 * g + j, most)) * DP + n * (DP / 16) + 4 * (u % ND));
+                    vr[i][4 * h + j] = *(const uint32_t*)(at + (uint32_t)(min(4 * g + j, most) * DP + n * (DP / 16)));
             }
         }
         const int tok = threadIdx.x & (TK - 1);
