@@ -724,7 +724,8 @@ struct Pairs {
     int lim[NT];                // tokens up to it are seen
     uint64_t mask[NT];          // drafted tokens that are seen
     float4_t o[NT][DP / 16];
-    float l[NT], ref[NT], top[NT], vlim[NT];
+    float l[NT], ref[NT];
+    float most[NT], vlim[NT];   // largest score and value scale that the reference allows
 };
 
 // The request, and the part of its tokens, that a workgroup of `pairs` pairs works on.
@@ -798,51 +799,63 @@ __device__ __forceinline__ void start(const AttendArgs& a, const Part& w, int he
         x.mask[t] = live && a.tree ? a.tree[w.first + i] : 0;
         x.l[t] = 0.0f;
         // nothing seen: a reference that any score moves
-        x.top[t] = -3e38f;      // largest score so far (of the four lanes of a column)
-        x.vlim[t] = 0x1p-88f;   // largest value scale its reference allows
+        x.most[t] = -3e38f;
+        x.vlim[t] = 0x1p-88f;
         x.ref[t] = 3e38f;
 #pragma unroll
         for (int j = 0; j < DP / 16; ++j) x.o[t][j] = float4_t{0, 0, 0, 0};
     }
 }
 
+// The largest of a lane's eight value scales, as the bits of a float: they are not
+// negative, so their bits order as they do, NaN above all.
+__device__ __forceinline__ int largest_bits(const float4_t (&v)[2]) {
+    int m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_int(v[j >> 2][j & 3]));
+    return m;
+}
+
 // Products of column t with 32 tokens from t0 on -> their weights times the value
-// scales, as the operand of the product with V.  all: every row sees all of them.
+// scales, as the operand of the product with V.  all: every row sees all of them;
+// vmax: largest_bits(vs).
 template <int DP, int NT>
 __device__ __forceinline__ half8_t weigh(const Part& w, Pairs<DP, NT>& x, int t, const float4_t (&s)[2], const float4_t (&ks)[2],
-                                         const float4_t (&vs)[2], int t0, bool all) {
+                                         const float4_t (&vs)[2], int vmax, int t0, bool all) {
     const int g = threadIdx.x >> 4 & 3;
-    float u[8], v[8], mx = -INFINITY, vmax = 0.0f;
+    float u[8], v[8], mx = -INFINITY;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         u[j] = s[j >> 2][j & 3] * ks[j >> 2][j & 3];
         v[j] = vs[j >> 2][j & 3];
     }
     if (!all) {
+        int stop = w.stop;
+        asm volatile("" : "+s"(stop));    // keeps what follows in here: the compiler moves it to every tile
+        vmax = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int tok = t0 + 16 * (j >> 2) + 4 * g + (j & 3);
             const int drafted = (int)(x.mask[t] >> ((tok - w.context) & 63)) & 1;
-            const bool sees = (tok < w.stop) & ((tok <= x.lim[t]) | drafted);
+            const bool sees = (tok < stop) & ((tok <= x.lim[t]) | drafted);
             u[j] = sees ? u[j] : -INFINITY;
             v[j] = sees ? v[j] : 0.0f;
+            vmax = max(vmax, __float_as_int(v[j]));
         }
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        mx = fmaxf(mx, u[j]);
-        vmax = fmaxf(vmax, v[j]);
-    }
+    for (int j = 0; j < 8; ++j) mx = fmaxf(mx, u[j]);
     // scores up to 2^6 above the reference's, value scales up to 4 above its, so that
     // weights of up to 2^14 fit a 16-bit float and all but those 2^-20 below the largest
     // keep its 11 bits
     mx *= x.f[t];
-    if (__any(mx > x.top[t] + 6.0f || vmax > x.vlim[t])) {
-        x.top[t] = fmaxf(x.top[t], column_max(mx));
-        const float most = column_max(vmax);
+    if (__any(mx > x.most[t] || vmax > __float_as_int(x.vlim[t]))) {
+        const float top = fmaxf(x.most[t] - 6.0f, column_max(mx));
+        const float most = column_max(__int_as_float(vmax));      // of those that are numbers
         if (most > x.vlim[t]) x.vlim[t] = ldexpf(1.0f, min(__builtin_amdgcn_frexp_expf(most), 100) + 2);
-        const float now = 8.0f - __builtin_amdgcn_logf(x.vlim[t]) - x.top[t];
+        const float now = 8.0f - __builtin_amdgcn_logf(x.vlim[t]) - top;
         const float by = __builtin_amdgcn_exp2f(now - x.ref[t]);
+        x.most[t] = top + 6.0f;
         x.ref[t] = now;
         x.l[t] *= by;
 #pragma unroll
@@ -1002,9 +1015,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend
             }
         }
         const bool all = t0 + 32 <= min(w.plain, w.stop);
+        const int vmax = largest_bits(x.vs);
         half8_t p[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) p[t] = weigh<DP, NT>(w, q, t, s[t], x.ks, x.vs, t0, all);
+        for (int t = 0; t < NT; ++t) p[t] = weigh<DP, NT>(w, q, t, s[t], x.ks, x.vs, vmax, t0, all);
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
             uint32_t words[8];
@@ -1080,17 +1094,20 @@ __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend
     }
 }
 
-// The same for many pairs (trees, chunks of a prompt): 16 NT a wave, their four waves
-// share the tokens.  A tile of TK tokens is read once, becomes 16-bit floats once and goes
-// to LDS in the order of the products' operands (16 bytes a lane, no conflicts), one tile
-// ahead of the products; its codes are in flight one further ahead.
-template <int FMT, int DP, int NT>
-__global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs a) {
-    constexpr int ND = DP / 64, MT = DP / 16, TK = DP <= 128 ? 64 : 32, PARTS = TK / 16;
-    constexpr int KU = PARTS * ND, KW = (KU + 3) / 4;          // 16-byte pieces of K, of them a wave's
-    constexpr int VU = PARTS / 2 * ND, VW = (VU + 3) / 4;      // words of V for 32 tokens, of them a wave's
-    __shared__ half8_t ks_[2][PARTS][2 * ND][64];   // part, step of 32 dimensions
-    __shared__ half8_t vs_[2][PARTS / 2][MT][64];   // 32 tokens, 16 dimensions
+// The same for many pairs (trees, chunks of a prompt): 16 NT a wave, and the WAVES share
+// the tokens.  A tile of TK tokens is read once, becomes 16-bit floats once and goes to
+// LDS in the order of the products' operands (16 bytes a lane, no conflicts), one tile
+// ahead of the products; the codes of the two tiles after it are in flight.  Where a workgroup's
+// pairs need half its waves or fewer, the others take every second 32 tokens of them, and
+// the two sums are joined at the end.
+template <int FMT, int DP, int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void attend_rows_kernel(AttendArgs a) {
+    constexpr int ND = DP / 64, MT = DP / 16, TK = 64, PARTS = TK / 16;
+    constexpr int KU = PARTS * ND, VU = PARTS / 2 * ND;   // 16-byte pieces of K, words of V for 32 tokens
+    // four waves take both, eight one or the other: about the same work each
+    constexpr int KW = KU / 4, VW = (VU + 3) / 4;         // a wave's
+    __shared__ half8_t ks_[2][PARTS][2 * ND][64];         // part, step of 32 dimensions
+    __shared__ half8_t vs_[2][PARTS / 2][MT][64];         // 32 tokens, 16 dimensions
     __shared__ __attribute__((aligned(16))) float scale[2][2][TK];
     const CacheArgs& c = a.c;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -1100,105 +1117,111 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs a) 
     const int split = blockIdx.x, head = blockIdx.y % c.heads, block = blocks - 1 - blockIdx.y / c.heads, r = blockIdx.z;
     Part w;
     if (!part_of(a, r, block, split, w)) return;
+    const bool halves = min(w.pairs - w.pair0, a.block_pairs) <= 8 * NT * WAVES;
     Pairs<DP, NT> q;
-    const int pair_from = w.pair0 + 16 * NT * wave;
+    const int pair_from = w.pair0 + 16 * NT * (halves ? wave >> 1 : wave);
     start<DP, NT>(a, w, head, pair_from, q);
 
     const int tiles = (w.stop - w.begin + TK - 1) / TK;
     const int last_part = (w.end - 1) >> 4;
     int page_of = 0;                    // lane i: the page of the i-th part from the last load
 
-    uint4_t kr[KW];
-    uint32_t vr[VW][8];
-    float sr = 0.0f;
-    auto load = [&](int it) {
+    const int vw = wave & 3;
+    const bool has_k = WAVES == 4 || wave >= 4, has_v = (WAVES == 4 || wave < 4) && vw < VU;
+    struct Codes {
+        uint4_t k[KW];
+        uint32_t v[VW][8];
+        float s;
+    } x[2];
+    auto load = [&](int it, Codes& x) {
         constexpr int TILES = 64 / PARTS;
         if (it % TILES == 0) page_of = page_of_part(c, r, min((w.begin >> 4) + it * PARTS + lane, last_part));
         const int in = it % TILES * PARTS, part0 = (w.begin >> 4) + it * PARTS;
+        if (has_k) {
 #pragma unroll
-        for (int i = 0; i < KW; ++i) {
-            const int u = wave + 4 * i, h = u / ND;
-            if (KU % 4 && u >= KU) break;
-            const int64_t slot = part_slot(c, __builtin_amdgcn_readlane(page_of, in + h), head, min(part0 + h, last_part));
-            kr[i] = *(const uint4_t*)(c.k + slot * DP + 16 * (u % ND) + (uint32_t)(n * DP + g * (DP / 4)));
+            for (int i = 0; i < KW; ++i) {
+                const int u = vw + 4 * i, h = u / ND;
+                const int64_t slot = part_slot(c, __builtin_amdgcn_readlane(page_of, in + h), head, min(part0 + h, last_part));
+                x.k[i] = *(const uint4_t*)(c.k + slot * DP + 16 * (u % ND) + (uint32_t)(n * DP + g * (DP / 4)));
+            }
         }
+        if (has_v) {
 #pragma unroll
-        for (int i = 0; i < VW; ++i) {
-            const int u = wave + 4 * i;
-            if (VU % 4 && u >= VU) break;
+            for (int i = 0; i < VW; ++i) {
+                const int u = vw + 4 * i;
+                if (u >= VU) break;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int p = 2 * (u / ND) + h, part = min(part0 + p, last_part);
-                const int64_t slot = part_slot(c, __builtin_amdgcn_readlane(page_of, in + p), head, part);
-                const uint8_t* at = c.v + slot * DP + 4 * (u % ND);
-                const int most = min(15, w.end - 1 - (part << 4));      // as in attend_kernel
+                for (int h = 0; h < 2; ++h) {
+                    const int p = 2 * (u / ND) + h, part = min(part0 + p, last_part);
+                    const int64_t slot = part_slot(c, __builtin_amdgcn_readlane(page_of, in + p), head, part);
+                    const uint8_t* at = c.v + slot * DP + 4 * (u % ND);
+                    const int most = min(15, w.end - 1 - (part << 4));      // as in attend_kernel
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    vr[i][4 * h + j] = *(const uint32_t*)(at + (uint32_t)(min(4 * g + j, most) * DP + n * (DP / 16)));
+                    for (int j = 0; j < 4; ++j)
+                        x.v[i][4 * h + j] = *(const uint32_t*)(at + (uint32_t)(min(4 * g + j, most) * DP + n * (DP / 16)));
+                }
             }
         }
         const int tok = threadIdx.x & (TK - 1);
         const int page = __shfl(page_of, in + (tok >> 4), 64);
         if (threadIdx.x < 2 * TK)
-            sr = (threadIdx.x < TK ? c.ks : c.vs)[part_slot(c, page, head, min(part0 + (tok >> 4), last_part)) + (tok & 15)];
+            x.s = (threadIdx.x < TK ? c.ks : c.vs)[part_slot(c, page, head, min(part0 + (tok >> 4), last_part)) + (tok & 15)];
     };
-    auto stage = [&](int b) {
+    auto stage = [&](int b, const Codes& x) {
+        if (has_k) {
 #pragma unroll
-        for (int i = 0; i < KW; ++i) {
-            const int u = wave + 4 * i;
-            if (KU % 4 && u >= KU) break;
-            ks_[b][u / ND][2 * (u % ND)][lane] = k_operand<FMT>(kr[i][0], kr[i][1]);
-            ks_[b][u / ND][2 * (u % ND) + 1][lane] = k_operand<FMT>(kr[i][2], kr[i][3]);
+            for (int i = 0; i < KW; ++i) {
+                const int u = vw + 4 * i;
+                ks_[b][u / ND][2 * (u % ND)][lane] = k_operand<FMT>(x.k[i][0], x.k[i][1]);
+                ks_[b][u / ND][2 * (u % ND) + 1][lane] = k_operand<FMT>(x.k[i][2], x.k[i][3]);
+            }
         }
+        if (has_v) {
 #pragma unroll
-        for (int i = 0; i < VW; ++i) {
-            const int u = wave + 4 * i;
-            if (VU % 4 && u >= VU) break;
-            half8_t v[4];
-            v_operands<FMT>(vr[i], v);
+            for (int i = 0; i < VW; ++i) {
+                const int u = vw + 4 * i;
+                if (u >= VU) break;
+                half8_t v[4];
+                v_operands<FMT>(x.v[i], v);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) vs_[b][u / ND][4 * (u % ND) + j][lane] = v[j];
+                for (int j = 0; j < 4; ++j) vs_[b][u / ND][4 * (u % ND) + j][lane] = v[j];
+            }
         }
-        if (threadIdx.x < 2 * TK) scale[b][threadIdx.x / TK][threadIdx.x & (TK - 1)] = sr;
+        if (threadIdx.x < 2 * TK) scale[b][threadIdx.x / TK][threadIdx.x & (TK - 1)] = x.s;
     };
 
     // tokens that the wave's rows may see
     const int wave_last = min(pair_from + 16 * NT, w.pairs) - 1;
     const int wave_stop = pair_from >= w.pairs ? w.begin : a.tree ? w.stop : min(w.stop, w.context + wave_last / a.group + 1);
-    if (tiles > 0) {
-        load(0);
-        stage(0);
-        if (tiles > 1) load(1);
-        __syncthreads();
-    }
-    for (int it = 0; it < tiles; ++it) {
-        const int b = it & 1, t0 = w.begin + it * TK;
+    auto use = [&](int it, int b) {
+        const int t0 = w.begin + it * TK;
         if (t0 < wave_stop) {
             const bool all = t0 + TK <= min(w.plain, w.stop);
 #pragma unroll
             for (int h = 0; h < PARTS / 2; ++h) {
+                if (halves && h != (wave & 1)) continue;
                 float4_t s[NT][2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = float4_t{0, 0, 0, 0};
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) s[t][i] = float4_t{0, 0, 0, 0};
+                for (int e = 0; e < 2 * ND; ++e)
 #pragma unroll
-                    for (int e = 0; e < 2 * ND; ++e) {
+                    for (int i = 0; i < 2; ++i) {
                         const half8_t k = ks_[b][2 * h + i][e][lane];
 #pragma unroll
                         for (int t = 0; t < NT; ++t)
                             s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q.q[t][e].v, s[t][i], 0, 0, 0);
                     }
-                }
                 float4_t ks[2], vs[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     ks[i] = *(const float4_t*)&scale[b][0][32 * h + 16 * i + 4 * g];
                     vs[i] = *(const float4_t*)&scale[b][1][32 * h + 16 * i + 4 * g];
                 }
+                const int vmax = largest_bits(vs);
                 half8_t p[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) p[t] = weigh<DP, NT>(w, q, t, s[t], ks, vs, t0 + 32 * h, all);
+                for (int t = 0; t < NT; ++t) p[t] = weigh<DP, NT>(w, q, t, s[t], ks, vs, vmax, t0 + 32 * h, all);
 #pragma unroll
                 for (int j = 0; j < MT; ++j) {
                     const half8_t v = vs_[b][h][j][lane];
@@ -1207,14 +1230,58 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs a) 
                 }
             }
         }
-        if (it + 1 < tiles) stage(b ^ 1);
-        if (it + 2 < tiles) load(it + 2);
+    };
+    if (tiles > 0) {
+        load(0, x[0]);
+        if (tiles > 1) load(1, x[1]);
+        stage(0, x[0]);
+        if (tiles > 2) load(2, x[0]);
+        __syncthreads();
+    }
+    for (int it = 0; it < tiles; it += 2) {
+        use(it, 0);
+        if (it + 1 >= tiles) break;
+        stage(1, x[1]);
+        if (it + 3 < tiles) load(it + 3, x[1]);
+        __syncthreads();
+        use(it + 1, 1);
+        if (it + 2 >= tiles) break;
+        stage(0, x[0]);
+        if (it + 4 < tiles) load(it + 4, x[0]);
         __syncthreads();
     }
 
 #pragma unroll
+    for (int t = 0; t < NT; ++t) q.l[t] = column_sum(q.l[t]);
+    if (halves) {
+        // the odd wave's sums to the even one's, a column and a row of outputs at a time,
+        // through the memory of the tiles
+        float4_t* half = (float4_t*)&ks_[0][0][0][0] + (wave >> 1) * 64;
+        float2* half_cl = (float2*)&scale[0][0][0] + (wave >> 1) * 16;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            __syncthreads();
+            if ((wave & 1) && g == 0) half_cl[n] = float2{q.ref[t], q.l[t]};
+            __syncthreads();
+            const float2 cl = half_cl[n];
+            const float ref = fminf(cl.x, q.ref[t]);
+            const float by = __builtin_amdgcn_exp2f(ref - q.ref[t]), other = __builtin_amdgcn_exp2f(ref - cl.x);
+            if (!(wave & 1)) {
+                q.l[t] = q.l[t] * by + cl.y * other;
+                q.ref[t] = ref;
+            }
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                __syncthreads();
+                if (wave & 1) half[lane] = q.o[t][j];
+                __syncthreads();
+                if (!(wave & 1)) q.o[t][j] = q.o[t][j] * by + half[lane] * other;
+            }
+        }
+        if (wave & 1) return;
+    }
+#pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const float sum = column_sum(q.l[t]);
         const int pair = pair_from + 16 * t + n;
         if (pair >= w.pairs) continue;
         // the lane's dimensions are (4 g + i) MT + j, so two i hold MT / 4 runs of eight
@@ -1225,56 +1292,47 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(AttendArgs a) 
                 float z[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) z[k] = q.o[t][(m + k) % MT][i + (m + k) / MT];
-                put_out<DP>(a, w, split, head, pair, (4 * g + i) * MT + m, z, sum, q.ref[t]);
+                put_out<DP>(a, w, split, head, pair, (4 * g + i) * MT + m, z, q.l[t], q.ref[t]);
             }
     }
 }
 
-// Joins the parts of a (row, head) pair that was split over tokens: a workgroup a pair,
-// every fourth part a wave.
+// Joins the parts of a (row, head) pair that was split over tokens: a wave a pair, the
+// heads of a row four by four.
 template <int DP>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
-    constexpr int V = DP / 64;
-    __shared__ float o_sum[kWaves][DP];
-    __shared__ float l_sum[kWaves];
+    constexpr int V = DP / 64;      // dimensions a lane sums: lane, lane + 64, ...
     const CacheArgs& c = a.c;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int i = blockIdx.x, qh = blockIdx.y, r = blockIdx.z;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i = blockIdx.x, qh = blockIdx.y * kWaves + wave, r = blockIdx.z;
     int64_t first;
     int rows, length;
-    if (!request_of(c, r, first, rows, length) || i >= rows) return;
+    if (qh >= a.q_heads || !request_of(c, r, first, rows, length) || i >= rows) return;
     // the tokens the row's workgroup saw: those of its block's last row
     const int end = a.tree ? length : length - rows + block_last_row(a, i, qh % a.group, rows) + 1;
     if (a.chunk >= end) return;
     const int parts = (end + a.chunk - 1) / a.chunk;
     const int64_t stride = c.rows * a.q_heads, global = (first + i) * a.q_heads + qh;
-    float m = 3e38f;
-    for (int k = lane; k < parts; k += 64) m = fminf(m, a.part_cl[k * stride + global].x);
-    for (int k = 32; k; k >>= 1) m = fminf(m, __shfl_xor(m, k, 64));
-    float o[V] = {}, l = 0.0f;
-#pragma unroll 4
-    for (int k = wave; k < parts; k += kWaves) {
+    float ref = 3e38f;
+    for (int k = lane; k < parts; k += 64) ref = fminf(ref, a.part_cl[k * stride + global].x);
+    for (int k = 32; k; k >>= 1) ref = fminf(ref, __shfl_xor(ref, k, 64));
+    float o[V] = {}, sum = 0.0f;
+#pragma unroll 8
+    for (int k = 0; k < parts; ++k) {
         const float2 cl = a.part_cl[k * stride + global];
-        const float by = __builtin_amdgcn_exp2f(m - cl.x);
-        const float* src = a.part_o + (k * stride + global) * DP + lane * V;
-        l = fmaf(cl.y, by, l);
+        const float by = __builtin_amdgcn_exp2f(ref - cl.x);
+        const float* src = a.part_o + (k * stride + global) * DP + lane;
+        sum = fmaf(cl.y, by, sum);
 #pragma unroll
-        for (int j = 0; j < V; ++j) o[j] = fmaf(src[j], by, o[j]);
+        for (int j = 0; j < V; ++j) o[j] = fmaf(src[64 * j], by, o[j]);
     }
-#pragma unroll
-    for (int j = 0; j < V; ++j) o_sum[wave][lane * V + j] = o[j];
-    if (lane == 0) l_sum[wave] = l;
-    __syncthreads();
-    const float sum = (l_sum[0] + l_sum[1]) + (l_sum[2] + l_sum[3]);
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const int d = threadIdx.x * 8;
-    if (d < DP) {
-        float z[8];
+    uint16_t* y = (uint16_t*)a.out.d + (first + i) * a.out.row + (int64_t)qh * a.out.head;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = (o_sum[0][d + j] + o_sum[1][d + j]) + (o_sum[2][d + j] + o_sum[3][d + j]);
-        store8(a, (first + i) * a.out.row + (int64_t)qh * a.out.head, d, z, inv);
-        if (d == 0 && a.lse) a.lse[global] = sum == 0.0f ? -INFINITY : (__builtin_amdgcn_logf(sum) - m) * kLn2;
-    }
+    for (int j = 0; j < V; ++j)
+        if (lane + 64 * j < c.dim)
+            y[lane + 64 * j] = a.half ? __builtin_bit_cast(uint16_t, (_Float16)(o[j] * inv)) : __builtin_bit_cast(uint16_t, (__bf16)(o[j] * inv));
+    if (a.lse && lane == 0) a.lse[global] = sum == 0.0f ? -INFINITY : (__builtin_amdgcn_logf(sum) - ref) * kLn2;
 }
 
 // ---------------------------------------------------------------------------
@@ -1448,11 +1506,13 @@ int cache_copy(orloj_worker* w, const orloj_cache* cache, const orloj_batch* bat
 // Launches `kernel` over blocks of block_pairs pairs, split over tokens where there are
 // few of them, and the join of the splits.
 template <int DP>
-int attend_blocks(orloj_worker* w, AttendArgs& a, const char* what, void (*kernel)(AttendArgs), int block_pairs, int per_unit) {
+int attend_blocks(orloj_worker* w, AttendArgs& a, const char* what, void (*kernel)(AttendArgs), int threads, int block_pairs,
+                  int per_unit) {
     const int64_t pairs = (int64_t)a.c.max_rows * a.group, blocks = (pairs + block_pairs - 1) / block_pairs;
     a.block_pairs = block_pairs;
     const int64_t groups = (int64_t)a.c.requests * a.c.heads * blocks;
-    // per_unit workgroups a unit where there are fewer, from at least 256 tokens each
+    // per_unit workgroups a unit where there are fewer, from at least 256 tokens each:
+    // as many as a unit holds at once
     const int64_t want = (per_unit * (int64_t)w->ctx->n_cu + groups - 1) / groups;
     const int64_t most = std::max<int64_t>(1, (a.c.max_length + 255) / 256);
     const int64_t parts = std::min(want, most);
@@ -1468,21 +1528,24 @@ int attend_blocks(orloj_worker* w, AttendArgs& a, const char* what, void (*kerne
         a.part_o = (float*)p;
         a.part_cl = (float2*)(a.part_o + n * DP);
     }
-    if (int rc = launch(w, what, kernel, dim3(splits, (unsigned)(blocks * a.c.heads), a.c.requests), kThreads, a)) return rc;
+    if (int rc = launch(w, what, kernel, dim3(splits, (unsigned)(blocks * a.c.heads), a.c.requests), threads, a)) return rc;
     if (splits == 1) return ORLOJ_OK;
-    return launch(w, "attend_join_kernel", attend_join_kernel<DP>, dim3(a.c.max_rows, a.q_heads, a.c.requests), kThreads, a);
+    return launch(w, "attend_join_kernel", attend_join_kernel<DP>,
+                  dim3(a.c.max_rows, (a.q_heads + kWaves - 1) / kWaves, a.c.requests), kThreads, a);
 }
 
 template <int FMT, int DP>
 int attend_dim(orloj_worker* w, AttendArgs& a) {
     const int64_t pairs = (int64_t)a.c.max_rows * a.group;
-    if (pairs <= 16) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, DP, 1>, 16, 4);
+    if (pairs <= 16) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, DP, 1>, kThreads, 16, 2);
     // beyond 128 dimensions the registers hold the sums of 16 pairs a wave
     if constexpr (DP <= 128) {
-        if (pairs <= 32) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, DP, 2>, 32, 4);
-        if (pairs > 64) return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, DP, 2>, 128, 4);
+        if (pairs <= 32) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, DP, 2>, kThreads, 32, 2);
+        if (pairs > 128) return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, DP, 2, 8>, 512, 256, 2);
+        return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, DP, 2, 4>, kThreads, 128, 2);
+    } else {
+        return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, DP, 1, 8>, 512, 128, 2);
     }
-    return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, DP, 1>, 64, 4);
 }
 
 template <int FMT>
