@@ -528,18 +528,15 @@ __device__ __forceinline__ bool request_of(const CacheArgs& c, int r, int64_t& f
     return !bad;
 }
 
-// Request and position of a row, found by the 16 lanes of a group together:
-// each round's 16 probes cut the candidates to a sixteenth.
+// Request and position of a row, found by a wave's lanes together: each round's 64 probes
+// cut the candidates to a 64th.
 __device__ __forceinline__ bool place_of_row(const CacheArgs& c, int64_t row, int& req, int& pos) {
-    const int lane = threadIdx.x & 63, sub = lane & 15;
+    const int lane = threadIdx.x & 63;
     int lo = 0, n = c.requests;            // the request is in [lo, lo + n)
     while (n > 1) {
-        const int step = (n + 15) >> 4;
-        const int p = lo + (sub + 1) * step;   // first row of request p
-        const bool past = p < lo + n && c.off[p] <= row;
-        const uint64_t m = __ballot(past) >> (lane & 48) & 0xffff;
-        const int k = __popcll(m);
-        const int from = lo + k * step;
+        const int step = (n + 63) >> 6;
+        const int p = lo + (lane + 1) * step;
+        const int from = lo + step * __popcll(__ballot(p < lo + n && c.off[p] <= row));
         n = min(step, lo + n - from);
         lo = from;
     }
@@ -555,24 +552,6 @@ __device__ __forceinline__ bool place_of_row(const CacheArgs& c, int64_t row, in
     return true;
 }
 
-// Offset of a token's slot among all (page, head, slot) triples, -1 where the
-// table is wrong.
-__device__ __forceinline__ int64_t slot_of(const CacheArgs& c, int req, int pos, int head) {
-    const int p = c.table[(int64_t)req * c.max_pages + (pos >> c.shift)];
-    if (p < 0 || p >= c.pages) {
-        atomicOr(c.err, kErrPage);
-        return -1;
-    }
-    return (((int64_t)p * c.heads + head) << c.shift) + (pos & (c.page - 1));
-}
-
-__device__ __forceinline__ uint8_t to_fp8(float x) {
-    return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false);
-}
-__device__ __forceinline__ float from_code(int format, uint8_t b) {
-    return format == ORLOJ_CACHE_INT8 ? (float)(int8_t)b : __builtin_amdgcn_cvt_f32_fp8(b, 0);
-}
-
 struct Vectors {
     void* d;
     int64_t row, head;
@@ -581,64 +560,194 @@ struct Vectors {
 struct CopyArgs {
     CacheArgs c;
     Vectors k, v;
+    int chunks;      // of kVectors vectors in a row
 };
 
-// 16 lanes a vector, 16 vectors a workgroup.
-template <class E>
-__global__ __launch_bounds__(kThreads) void cache_write_kernel(CopyArgs a) {
+// A wave moves kVectors of the keys' and values' vectors of one row, so that a row is
+// looked up once for them: 16 lanes a vector, pad / 16 adjacent elements a lane, the
+// loads of all of them before the first is used.
+constexpr int kVectors = 8;
+
+// A lane's share of one vector: the vector's slot among all (page, head, slot) triples, and
+// where its elements are.  False past the row's last vector.
+struct Share {
+    int64_t slot;
+    bool is_k;
+    int64_t at;
+};
+__device__ __forceinline__ bool share_of(const CopyArgs& a, int64_t row, int page, int pos, int i, Share& s) {
     const CacheArgs& c = a.c;
-    using T = typename E::T;
-    const int sub = threadIdx.x & 15;
-    const int64_t i = (int64_t)blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
-    const int64_t row = i / (2 * c.heads);
-    const int which = (int)(i - row * 2 * c.heads);
-    const int head = which % c.heads;
-    if (row >= c.rows) return;
-    int req, pos;
-    if (!place_of_row(c, row, req, pos)) return;
-    const int64_t slot = slot_of(c, req, pos, head);
-    if (slot < 0) return;
-    const Vectors& from = which < c.heads ? a.k : a.v;
-    const T* x = (const T*)from.d + row * from.row + head * from.head;
-    float amax = 0.0f;
-    for (int d = sub; d < c.dim; d += 16) {
-        const float y = fabsf(E::up(x[d]));
-        amax = y > amax || y != y ? y : amax;
-    }
-    for (int m = 8; m; m >>= 1) {
-        const float o = __shfl_xor(amax, m, 64);
-        amax = o > amax || o != o ? o : amax;
-    }
-    const bool bad = !(amax < INFINITY), low = amax < kTiny;
-    const float top = c.format == ORLOJ_CACHE_INT8 ? 127.0f : 448.0f;
-    const float inv = (1.0f / (bad || low ? 1.0f : amax)) * top;
-    uint8_t* code = (which < c.heads ? c.k : c.v) + slot * c.pad;
-    for (int d = sub; d < c.pad; d += 16) {
-        const float y = d < c.dim && !bad && !low ? E::up(x[d]) * inv : 0.0f;
-        code[d] = c.format == ORLOJ_CACHE_INT8 ? (uint8_t)(int8_t)rintf(y) : to_fp8(y);
-    }
-    if (sub == 0) (which < c.heads ? c.ks : c.vs)[slot] = bad ? NAN : low ? 0.0f : amax * (1.0f / top);
+    if (i >= 2 * c.heads) return false;
+    s.is_k = i < c.heads;
+    const int head = s.is_k ? i : i - c.heads;
+    s.slot = (((int64_t)page * c.heads + head) << c.shift) + (pos & (c.page - 1));
+    const Vectors& v = s.is_k ? a.k : a.v;
+    s.at = row * v.row + head * v.head;
+    return true;
+}
+// The wave's row and first vector, the row's page and position; false: nothing to do.
+__device__ __forceinline__ bool wave_row(const CopyArgs& a, int64_t& row, int& from, int& page, int& pos) {
+    const int64_t i = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    row = i / a.chunks;
+    from = (int)(i - row * a.chunks) * kVectors;
+    int req;
+    if (row >= a.c.rows || !place_of_row(a.c, row, req, pos)) return false;
+    page = a.c.table[(int64_t)req * a.c.max_pages + (pos >> a.c.shift)];
+    if (page >= 0 && page < a.c.pages) return true;
+    atomicOr(a.c.err, kErrPage);
+    return false;
 }
 
-template <class E>
-__global__ __launch_bounds__(kThreads) void cache_read_kernel(CopyArgs a) {
+typedef uint16_t ushort4_u __attribute__((ext_vector_type(4), aligned(2)));
+typedef float float4_u __attribute__((ext_vector_type(4), aligned(4)));
+
+// N adjacent elements from p on, of which `count` exist.
+template <class E, int N>
+__device__ __forceinline__ void load_elements(const typename E::T* p, int count, float (&x)[N]) {
+    if (count >= N) {
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+            if constexpr (sizeof(typename E::T) == 4) {
+                const float4_u v = *(const float4_u*)(p + e);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[e + j] = v[j];
+            } else {
+                const ushort4_u v = *(const ushort4_u*)(p + e);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint16_t u = v[j];
+                    x[e + j] = E::up(__builtin_bit_cast(typename E::T, u));
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = e < count ? E::up(p[e]) : 0.0f;
+    }
+}
+template <class E, int N>
+__device__ __forceinline__ void store_elements(typename E::T* p, int count, const float (&x)[N]) {
+    if (count >= N) {
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+            if constexpr (sizeof(typename E::T) == 4) {
+                *(float4_u*)(p + e) = float4_u{x[e], x[e + 1], x[e + 2], x[e + 3]};
+            } else {
+                ushort4_u v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = __builtin_bit_cast(uint16_t, E::down(x[e + j]));
+                *(ushort4_u*)(p + e) = v;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < count) p[e] = E::down(x[e]);
+    }
+}
+
+// Bound by its bytes: 2 D in and D + 4 out a vector (16-bit activations).
+template <class E, int FMT, int ND>
+__global__ __launch_bounds__(kThreads) void cache_write_kernel(CopyArgs a) {
+    constexpr int N = 4 * ND, ROUNDS = kVectors / 4;
     const CacheArgs& c = a.c;
-    using T = typename E::T;
-    const int sub = threadIdx.x & 15;
-    const int64_t i = (int64_t)blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
-    const int64_t row = i / (2 * c.heads);
-    const int which = (int)(i - row * 2 * c.heads);
-    const int head = which % c.heads;
-    if (row >= c.rows) return;
-    int req, pos;
-    if (!place_of_row(c, row, req, pos)) return;
-    const int64_t slot = slot_of(c, req, pos, head);
-    if (slot < 0) return;
-    const Vectors& to = which < c.heads ? a.k : a.v;
-    T* x = (T*)to.d + row * to.row + head * to.head;
-    const uint8_t* code = (which < c.heads ? c.k : c.v) + slot * c.pad;
-    const float s = (which < c.heads ? c.ks : c.vs)[slot];
-    for (int d = sub; d < c.dim; d += 16) x[d] = E::down(from_code(c.format, code[d]) * s);
+    const int sub = threadIdx.x & 15, which = threadIdx.x >> 4 & 3;
+    int64_t row;
+    int from, page, pos;
+    if (!wave_row(a, row, from, page, pos)) return;
+    float x[ROUNDS][N];
+    Share s[ROUNDS];
+    bool has[ROUNDS];
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        has[r] = share_of(a, row, page, pos, from + 4 * r + which, s[r]);
+        if (has[r]) load_elements<E, N>((const typename E::T*)(s[r].is_k ? a.k : a.v).d + s[r].at + sub * N, c.dim - sub * N, x[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        if (!has[r]) continue;
+        // the largest magnitude, on its bits: NaN above infinity above the numbers
+        int m = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) m = max(m, __float_as_int(fabsf(x[r][e])));
+#pragma unroll
+        for (int k = 8; k; k >>= 1) m = max(m, __shfl_xor(m, k, 64));
+        const float amax = __int_as_float(m);
+        const bool bad = !(amax < INFINITY), low = amax < kTiny;
+        const float top = FMT == ORLOJ_CACHE_INT8 ? 127.0f : 448.0f;
+        const float inv = (1.0f / (bad || low ? 1.0f : amax)) * top;
+        uint32_t w[ND];
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            float y[4];
+            {
+#pragma clang fp contract(off)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = bad || low ? 0.0f : x[r][4 * d + j] * inv;
+            }
+            if (FMT == ORLOJ_CACHE_INT8) {
+                // 1.5 * 2^23 + y: y's nearest integer, ties to even, in the low bits (y itself
+                // rounded before, as defined: no fused multiply and add)
+#pragma clang fp contract(off)
+                uint32_t u[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) u[j] = __float_as_uint(y[j] + 12582912.0f);
+                w[d] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400u), __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), 0x05040100u);
+            } else {
+                int u = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+                w[d] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], u, true);
+            }
+        }
+        uint32_t* code = (uint32_t*)((s[r].is_k ? c.k : c.v) + s[r].slot * c.pad) + sub * ND;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) code[d] = w[d];
+        if (sub == 0) (s[r].is_k ? c.ks : c.vs)[s[r].slot] = bad ? NAN : low ? 0.0f : amax * (1.0f / top);
+    }
+}
+
+template <class E, int FMT, int ND>
+__global__ __launch_bounds__(kThreads) void cache_read_kernel(CopyArgs a) {
+    constexpr int N = 4 * ND, ROUNDS = kVectors / 4;
+    const CacheArgs& c = a.c;
+    const int sub = threadIdx.x & 15, which = threadIdx.x >> 4 & 3;
+    int64_t row;
+    int from, page, pos;
+    if (!wave_row(a, row, from, page, pos)) return;
+    uint32_t w[ROUNDS][ND];
+    float scale[ROUNDS];
+    Share s[ROUNDS];
+    bool has[ROUNDS];
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        has[r] = share_of(a, row, page, pos, from + 4 * r + which, s[r]);
+        if (!has[r]) continue;
+        const uint32_t* code = (const uint32_t*)((s[r].is_k ? c.k : c.v) + s[r].slot * c.pad) + sub * ND;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) w[r][d] = code[d];
+        scale[r] = (s[r].is_k ? c.ks : c.vs)[s[r].slot];
+    }
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        if (!has[r]) continue;
+        float x[N];
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            const int u = (int)w[r][d];
+            float y[4];
+            if (FMT == ORLOJ_CACHE_INT8) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = (float)(int8_t)(u >> 8 * j);
+            } else {
+                y[0] = __builtin_amdgcn_cvt_f32_fp8(u, 0);
+                y[1] = __builtin_amdgcn_cvt_f32_fp8(u, 1);
+                y[2] = __builtin_amdgcn_cvt_f32_fp8(u, 2);
+                y[3] = __builtin_amdgcn_cvt_f32_fp8(u, 3);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[4 * d + j] = y[j] * scale[r];
+        }
+        store_elements<E, N>((typename E::T*)(s[r].is_k ? a.k : a.v).d + s[r].at + sub * N, c.dim - sub * N, x);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -1476,6 +1585,22 @@ int vectors(orloj_worker* w, const orloj_vectors* v, int64_t rows, const char* n
     return ORLOJ_OK;
 }
 
+template <class E, int FMT, int ND>
+int copy_pages(orloj_worker* w, const CopyArgs& a, dim3 g, bool write) {
+    return write ? launch(w, "cache_write_kernel", cache_write_kernel<E, FMT, ND>, g, kThreads, a)
+                 : launch(w, "cache_read_kernel", cache_read_kernel<E, FMT, ND>, g, kThreads, a);
+}
+template <class E>
+int copy_as(orloj_worker* w, const CopyArgs& a, dim3 g, bool write) {
+    const bool i8 = a.c.format == ORLOJ_CACHE_INT8;
+    switch (a.c.pad / 64) {
+        case 1: return i8 ? copy_pages<E, ORLOJ_CACHE_INT8, 1>(w, a, g, write) : copy_pages<E, ORLOJ_CACHE_FP8, 1>(w, a, g, write);
+        case 2: return i8 ? copy_pages<E, ORLOJ_CACHE_INT8, 2>(w, a, g, write) : copy_pages<E, ORLOJ_CACHE_FP8, 2>(w, a, g, write);
+        case 3: return i8 ? copy_pages<E, ORLOJ_CACHE_INT8, 3>(w, a, g, write) : copy_pages<E, ORLOJ_CACHE_FP8, 3>(w, a, g, write);
+        default: return i8 ? copy_pages<E, ORLOJ_CACHE_INT8, 4>(w, a, g, write) : copy_pages<E, ORLOJ_CACHE_FP8, 4>(w, a, g, write);
+    }
+}
+
 int cache_copy(orloj_worker* w, const orloj_cache* cache, const orloj_batch* batch, int32_t dtype,
                const orloj_vectors* k, const orloj_vectors* v, bool write) {
     if (!w) return ORLOJ_E_INVALID;
@@ -1486,21 +1611,16 @@ int cache_copy(orloj_worker* w, const orloj_cache* cache, const orloj_batch* bat
     if (int rc = vectors(w, v, c.rows, "v", &a.v)) return rc;
     if (dtype != ORLOJ_F32 && dtype != ORLOJ_F16 && dtype != ORLOJ_BF16)
         return orloj_ctx_fail(w->ctx, ORLOJ_E_INVALID, "unknown dtype %d", dtype);
-    const int64_t groups = (c.rows * 2 * c.heads + kThreads / 16 - 1) / (kThreads / 16);
+    a.chunks = (2 * c.heads + kVectors - 1) / kVectors;
+    const int64_t groups = (c.rows * a.chunks + kWaves - 1) / kWaves;
     if (groups > INT32_MAX)
         return orloj_ctx_fail(w->ctx, ORLOJ_E_UNSUPPORTED, "%lld rows of %d heads are too many for one call",
                               (long long)c.rows, c.heads);
     if (int rc = enter(w)) return rc;
     if (c.rows == 0) return ORLOJ_OK;
     const dim3 g((unsigned)groups);
-    if (write) {
-        auto kernel = dtype == ORLOJ_F32 ? cache_write_kernel<F32> : dtype == ORLOJ_F16 ? cache_write_kernel<F16>
-                                                                                   : cache_write_kernel<BF16>;
-        return launch(w, "cache_write_kernel", kernel, g, kThreads, a);
-    }
-    auto kernel = dtype == ORLOJ_F32 ? cache_read_kernel<F32> : dtype == ORLOJ_F16 ? cache_read_kernel<F16>
-                                                                               : cache_read_kernel<BF16>;
-    return launch(w, "cache_read_kernel", kernel, g, kThreads, a);
+    return dtype == ORLOJ_F32 ? copy_as<F32>(w, a, g, write) : dtype == ORLOJ_F16 ? copy_as<F16>(w, a, g, write)
+                                                                                 : copy_as<BF16>(w, a, g, write);
 }
 
 // Launches `kernel` over blocks of block_pairs pairs, split over tokens where there are

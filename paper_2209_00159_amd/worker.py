@@ -60,20 +60,21 @@ class Worker:
 def _need(t, name, dtype, device):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if t.device != device:
+    if t.get_device() != device.index:
         raise ValueError(f"{name} must live on {device}, not {t.device}")
 
 
 def _rows(t, name, dtype, device, width):
     """Row stride of a [rows, width] matrix whose rows are contiguous."""
     _need(t, name, dtype, device)
-    if t.dim() != 2 or t.shape[1] != width:
-        raise ValueError(f"{name} must be [rows, {width}], not {list(t.shape)}")
-    if width > 1 and t.stride(1) != 1:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[1] != width:
+        raise ValueError(f"{name} must be [rows, {width}], not {list(shape)}")
+    if width > 1 and stride[1] != 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else width
+    return stride[0] if shape[0] > 1 else width
 
 
 def _vectors(t, name, dtype, device, rows, heads, dim):
@@ -81,9 +82,10 @@ def _vectors(t, name, dtype, device, rows, heads, dim):
     _need(t, name, dtype, device)
     if t.shape != (rows, heads, dim):
         raise ValueError(f"{name} must be {[rows, heads, dim]}, not {list(t.shape)}")
-    if dim > 1 and t.stride(2) != 1:
+    stride = t.stride()
+    if dim > 1 and stride[2] != 1:
         raise ValueError(f"{name} must have contiguous vectors")
-    return O.Vectors(t.data_ptr(), t.stride(0), t.stride(1))
+    return O.Vectors(t.data_ptr(), stride[0], stride[1])
 
 
 class Adapters:
@@ -203,7 +205,7 @@ class Cache:
         return cls(worker, k, v, ks, vs, head_dim)
 
     def _check_batch(self, batch: Batch):
-        if batch.device != self.worker.device:
+        if batch.device is not self.worker.device and batch.device != self.worker.device:
             raise ValueError(f"the batch must live on {self.worker.device}, not {batch.device}")
 
     def write(self, batch: Batch, k: torch.Tensor, v: torch.Tensor):

@@ -195,6 +195,31 @@ def test_cache(worker, fmt, dtype, dim, heads, page, requests):
         assert torch.equal(torch.nan_to_num(ps[~used], nan=7.0), torch.nan_to_num(before[n + "_scale"][~used], nan=7.0))
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_cache_codes_are_those_of_32_bit_arithmetic(worker, fmt, dtype):
+    """scale = amax (1 / top), code = x ((1 / amax) top) to the nearest, each step rounded to 32
+    bits: the same codes, ties and all."""
+    say("cache codes", fmt, dtype)
+    p = P.Paged([(0, 700)], 64, 4, 128, fmt, seed=3)
+    cache, batch = p.cache(W, worker), p.batch(W, worker)
+    x = torch.randn(700, 4, 128, generator=p.g).to(dtype)
+    x[::3] = (x[::3] * 8).round() / 8                 # many ties
+    cache.write(batch, x.to(worker.device), x.to(worker.device))
+    worker.sync()
+    f = x.float()
+    amax = f.abs().amax(-1)
+    top = torch.tensor(P.TOP[fmt])
+    inv = (torch.tensor(1.0) / amax) * top
+    y = f * inv[..., None]
+    want = y.round().to(torch.int8) if fmt == torch.int8 else y.to(torch.float8_e4m3fn)
+    for pool, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
+        for t in range(700):
+            page, slot = p.at(0, t)
+            assert torch.equal(pool[page, :, slot].cpu().view(torch.uint8), want[t].view(torch.uint8)), t
+            assert torch.equal(scale[page, :, slot].cpu(), amax[t] * (torch.tensor(1.0) / top))
+
+
 def test_cache_of_many_requests(worker):
     """A row's request is found among many, empty ones between them."""
     say("cache of many requests")
