@@ -95,6 +95,14 @@ struct AdaptArgs {
     int* err;
 };
 
+// The workgroup's item of a list of gridDim.x: workgroups go to the eight XCDs in turn, each
+// with an L2 of its own, so that neighbours in the list, which read the same weights, share
+// one.
+__device__ __forceinline__ int xcd_item() {
+    const int n = gridDim.x, id = blockIdx.x, xcd = id & 7, each = n >> 3, more = n & 7;
+    return xcd * each + min(xcd, more) + (id >> 3);
+}
+
 // Row t's adapter, -1 where it has none or one of rank 0.
 __device__ __forceinline__ int adapter_of(const AdaptArgs& a, int64_t t, int& rank) {
     int id = t < a.rows ? a.adapter[t] : -1;
@@ -127,8 +135,7 @@ __device__ __forceinline__ ushort8_t cut_piece(ushort8_t v, int at, int start, i
 
 // h = A_a x for 16 NT rows and up to 16 RT ranks: D = A_a X^T, ranks by rows, on
 // v_mfma_f32_16x16x32.  Both operands are contiguous along k, so a lane loads its
-// 16 bytes of each straight into the operand's registers (32 bytes a row and lane and
-// step of 64).  The four waves take 64 of each 256 elements; their sums meet in LDS,
+// 16 bytes of each straight into the operand's registers, 64 adjacent bytes a row.  The four waves take 64 of each 256 elements; their sums meet in LDS,
 // those of the splits of d_in in adapt_up_kernel.
 // The rows' distinct adapters: with NT = 1 (few rows) the z-th of the grid's z-th
 // workgroup, else one after the other (rows of a prompt share theirs).
@@ -138,7 +145,10 @@ __global__ __launch_bounds__(kThreads, RT * NT <= 16 ? 2 : 1) void adapt_down_ke
     __shared__ __attribute__((aligned(16))) float sum[ROWS][RANKS + 4];
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t t0 = (int64_t)blockIdx.x * ROWS;
+    // few rows: tiles by splits by distinct adapters; many: a list of tiles, each's splits together
+    const int item = NT == 1 ? 0 : xcd_item();
+    const int split = NT == 1 ? blockIdx.y : item % a.splits;
+    const int64_t t0 = (int64_t)(NT == 1 ? blockIdx.x : item / a.splits) * ROWS;
     int rank;
     const int id = adapter_of(a, lane < ROWS ? t0 + lane : a.rows, rank);
     uint64_t left = __ballot(id >= 0);
@@ -150,7 +160,7 @@ __global__ __launch_bounds__(kThreads, RT * NT <= 16 ? 2 : 1) void adapt_down_ke
         if (NT == 1 && z != (int)blockIdx.z) continue;
         const int ranks = __builtin_amdgcn_readlane(rank, lead);
         const uint16_t* w = (const uint16_t*)a.down + (int64_t)which * a.rank * a.d_in;
-        const int from = blockIdx.y * a.k_part, to = min(from + a.k_part, a.d_in);
+        const int from = split * a.k_part, to = min(from + a.k_part, a.d_in);
 
         const uint16_t *ap[RT], *xp[NT];
 #pragma unroll
@@ -160,7 +170,7 @@ __global__ __launch_bounds__(kThreads, RT * NT <= 16 ? 2 : 1) void adapt_down_ke
         float4_t acc[RT][NT] = {};
         ushort8_t av[2][RT], xv[2][NT];
         auto load = [&](int k, int s) {
-            const int at = k + 16 * g + 8 * s;
+            const int at = k + 32 * s + 8 * g;
 #pragma unroll
             for (int i = 0; i < RT; ++i) av[s][i] = *(const ushort8_u*)(ap[i] + at);
 #pragma unroll
@@ -187,7 +197,7 @@ __global__ __launch_bounds__(kThreads, RT * NT <= 16 ? 2 : 1) void adapt_down_ke
         if (k < to) {
 #pragma unroll 1
             for (int s = 0; s < 2; ++s) {
-                const int start = k + 16 * g + 8 * s, at = piece_at(start, a.d_in);
+                const int start = k + 32 * s + 8 * g, at = piece_at(start, a.d_in);
                 ushort8_t x[NT];
 #pragma unroll
                 for (int j = 0; j < NT; ++j) x[j] = cut_piece(*(const ushort8_u*)(xp[j] + at), at, start, a.d_in);
@@ -211,7 +221,7 @@ __global__ __launch_bounds__(kThreads, RT * NT <= 16 ? 2 : 1) void adapt_down_ke
             }
             __syncthreads();
         }
-        float* h = a.h + ((int64_t)blockIdx.y * a.rows + t0) * a.rank;
+        float* h = a.h + ((int64_t)split * a.rows + t0) * a.rank;
         for (int e = threadIdx.x; e < ROWS * a.rank; e += kThreads) {
             const int row = e / a.rank, r = e - row * a.rank;
             if (mine >> row & 1) h[e] = r < ranks ? sum[row][r] : 0.0f;
@@ -278,15 +288,16 @@ __device__ __forceinline__ void put_h(const AdaptArgs& a, int64_t t, bool live, 
     if (n == 0) *by = ldexpf(1.0f, ex);
 }
 
-// The operand of 64 outputs from o0 on: row m of product j is output 16 (m / 4) + 4 j +
-// m mod 4, so that a lane of the result holds 16 adjacent outputs of a row.
+// The operand of 64 outputs from o0 on: its rows are ordered so that a lane of the result
+// holds two runs of 8 adjacent outputs of a row, 32 apart, and the four lanes of a row 32
+// adjacent ones.
 template <int STEPS>
 __device__ __forceinline__ void load_up(const AdaptArgs& a, int which, int ranks, int o0, ushort8_t (&wv)[STEPS][4]) {
     const int n = threadIdx.x & 15, g = threadIdx.x >> 4 & 3;
     const uint16_t* w = (const uint16_t*)a.up + (int64_t)which * a.d_out * a.rank;
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-        const int o = min(o0 + 16 * (n >> 2) + 4 * m + (n & 3), a.d_out - 1);
+        const int o = min(o0 + 32 * (m >> 1) + 8 * (n >> 2) + 4 * (m & 1) + (n & 3), a.d_out - 1);
 #pragma unroll
         for (int e = 0; e < STEPS; ++e) {
             const uint16_t* p = w + (int64_t)o * a.rank;
@@ -323,26 +334,26 @@ __device__ __forceinline__ void product_up(const ushort8_t (&wv)[STEPS][4], cons
     }
 }
 
-// A lane's 16 outputs of a row, as two pieces; element by element in the last block of a
-// width that 64 does not divide.
+// A lane's 16 outputs of a row, as two pieces 32 apart; element by element in the last
+// block of a width that 64 does not divide.
 template <bool FULL>
 __device__ __forceinline__ void load_base(const AdaptArgs& a, int64_t t, int o0, ushort8_t (&v)[2]) {
-    const int o = o0 + (threadIdx.x >> 4 & 3) * 16;
+    const int o = o0 + (threadIdx.x >> 4 & 3) * 8;
     v[0] = v[1] = ushort8_t{0, 0, 0, 0, 0, 0, 0, 0};
     if (!a.base || t >= a.rows) return;
     const uint16_t* p = (const uint16_t*)a.base + t * a.bs;
     if (FULL) {
         v[0] = *(const ushort8_u*)(p + o);
-        v[1] = *(const ushort8_u*)(p + o + 8);
+        v[1] = *(const ushort8_u*)(p + o + 32);
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i >> 3][i & 7] = p[min(o + i, a.d_out - 1)];
+        for (int i = 0; i < 16; ++i) v[i >> 3][i & 7] = p[min(o + (i >> 3) * 32 + (i & 7), a.d_out - 1)];
     }
 }
 
 template <class E, bool FULL>
 __device__ __forceinline__ void put_y(const AdaptArgs& a, int64_t t, int o0, const float4_t (&d)[4], float f, const ushort8_t (&v)[2]) {
-    const int o = o0 + (threadIdx.x >> 4 & 3) * 16;
+    const int o = o0 + (threadIdx.x >> 4 & 3) * 8;
     uint16_t* y = (uint16_t*)a.y + t * a.ys;
     ushort8_t z[2];
 #pragma unroll
@@ -353,11 +364,11 @@ __device__ __forceinline__ void put_y(const AdaptArgs& a, int64_t t, int o0, con
     }
     if (FULL) {
         *(ushort8_u*)(y + o) = z[0];
-        *(ushort8_u*)(y + o + 8) = z[1];
+        *(ushort8_u*)(y + o + 32) = z[1];
     } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-            if (o + i < a.d_out) y[o + i] = z[i >> 3][i & 7];
+            if (o + (i >> 3) * 32 + (i & 7) < a.d_out) y[o + (i >> 3) * 32 + (i & 7)] = z[i >> 3][i & 7];
     }
 }
 
@@ -434,23 +445,24 @@ __global__ __launch_bounds__(kThreads) void adapt_up_few_kernel(AdaptArgs a) {
 
 // Many rows: 64 a workgroup, 64 outputs a wave of each block of 256; the rows' distinct
 // adapters (adjacent rows of a prompt share theirs) one after the other.
-template <class E, int STEPS>
+template <class E, int STEPS, int NT>
 __global__ __launch_bounds__(kThreads) void adapt_up_kernel(AdaptArgs a) {
-    constexpr int PITCH = 32 * STEPS + 8;
-    __shared__ __attribute__((aligned(16))) uint16_t hs[2][64][PITCH];
-    __shared__ float by[64];
+    constexpr int PITCH = 32 * STEPS + 8, ROWS = 16 * NT;
+    __shared__ __attribute__((aligned(16))) uint16_t hs[2][ROWS][PITCH];
+    __shared__ float by[ROWS];
     const int lane = threadIdx.x & 63, n = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t t0 = (int64_t)blockIdx.y * 64;
+    const int item = xcd_item(), across = ((a.d_out + 255) / 256 + a.blocks - 1) / a.blocks;
+    const int64_t t0 = (int64_t)(item / across) * ROWS;
     int rank;
-    const int id = adapter_of(a, t0 + lane, rank);
+    const int id = adapter_of(a, lane < ROWS ? t0 + lane : a.rows, rank);
     const uint64_t some = __ballot(id >= 0);
-    for (int row = threadIdx.x >> 4; row < 64; row += kThreads / 16)
+    for (int row = threadIdx.x >> 4; row < ROWS; row += kThreads / 16)
         put_h<E, STEPS>(a, t0 + row, some >> row & 1, hs[0][row], hs[1][row], &by[row]);
     __syncthreads();
 
     for (int b = 0; b < a.blocks; ++b) {
-        const int o0 = (blockIdx.x * a.blocks + b) * 256 + 64 * wave;
+        const int o0 = (item % across * a.blocks + b) * 256 + 64 * wave;
         if (o0 >= a.d_out) break;
         const bool whole = o0 + 64 <= a.d_out;
         for (uint64_t left = some; left;) {
@@ -461,11 +473,11 @@ __global__ __launch_bounds__(kThreads) void adapt_up_kernel(AdaptArgs a) {
             ushort8_t wv[STEPS][4];
             load_up<STEPS>(a, which, __builtin_amdgcn_readlane(rank, lead), o0, wv);
             if (whole) {
-                ushort8_t base[4][2];
+                ushort8_t base[NT][2];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) load_base<true>(a, t0 + 16 * j + n, o0, base[j]);
+                for (int j = 0; j < NT; ++j) load_base<true>(a, t0 + 16 * j + n, o0, base[j]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < NT; ++j) {
                     if (!(mine >> (16 * j) & 0xffff)) continue;
                     float4_t d[4];
                     product_up<E, STEPS>(wv, hs[0][16 * j + n], hs[1][16 * j + n], d);
@@ -473,7 +485,7 @@ __global__ __launch_bounds__(kThreads) void adapt_up_kernel(AdaptArgs a) {
                 }
             } else {
 #pragma unroll 1
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < NT; ++j) {
                     if (!(mine >> (16 * j) & 0xffff)) continue;
                     ushort8_t base[2];
                     load_base<false>(a, t0 + 16 * j + n, o0, base);
@@ -485,7 +497,7 @@ __global__ __launch_bounds__(kThreads) void adapt_up_kernel(AdaptArgs a) {
         }
         // rows without an adapter
 #pragma unroll 1
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < NT; ++j) {
             const int64_t t = t0 + 16 * j + n;
             if ((some >> (16 * j + n) & 1) || t >= a.rows) continue;
             const float4_t none[4] = {};
@@ -1518,14 +1530,14 @@ int adapt_tiles(orloj_worker* w, AdaptArgs& a) {
     const int rc = a.d_in < 8 ? launch(w, "adapt_down_narrow_kernel", adapt_down_narrow_kernel<E>,
                                        dim3((unsigned)((a.rows * a.rank + kThreads - 1) / kThreads)), kThreads, a)
                               : launch(w, "adapt_down_kernel", adapt_down_kernel<E, RT, NT>,
-                                       dim3(tiles, a.splits, slots), kThreads, a);
+                                       NT == 1 ? dim3(tiles, a.splits, slots) : dim3(tiles * a.splits), kThreads, a);
     if (rc) return rc;
     constexpr int STEPS = RT == 8 ? 4 : RT == 4 ? 2 : 1;
     if (NT == 1)
         return launch(w, "adapt_up_few_kernel", adapt_up_few_kernel<E, STEPS>, dim3((a.d_out + 63) / 64, tiles), kThreads, a);
     const int blocks = (a.d_out + 255) / 256;
     a.blocks = std::max(1, std::min(2, tiles * blocks / (2 * w->ctx->n_cu)));
-    return launch(w, "adapt_up_kernel", adapt_up_kernel<E, STEPS>, dim3((blocks + a.blocks - 1) / a.blocks, tiles), kThreads, a);
+    return launch(w, "adapt_up_kernel", adapt_up_kernel<E, STEPS, NT == 1 ? 4 : NT>, dim3((blocks + a.blocks - 1) / a.blocks * tiles), kThreads, a);
 }
 
 template <class E>
