@@ -1574,6 +1574,7 @@ int cache_args(orloj_worker* w, const orloj_cache* c, const orloj_batch* b, Cach
         return orloj_ctx_fail(x, ORLOJ_E_INVALID, "a size of the batch is negative");
     if (b->n_rows > INT32_MAX)
         return orloj_ctx_fail(x, ORLOJ_E_UNSUPPORTED, "n_rows %lld > 2^31 - 1", (long long)b->n_rows);
+    if (b->max_length > 1 << 30) return orloj_ctx_fail(x, ORLOJ_E_UNSUPPORTED, "max_length %d > 2^30", b->max_length);
     if (b->n_requests == 0 && b->n_rows > 0)
         return orloj_ctx_fail(x, ORLOJ_E_INVALID, "%lld rows of no requests", (long long)b->n_rows);
     if (b->n_rows > 0) {

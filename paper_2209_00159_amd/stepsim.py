@@ -1,0 +1,192 @@
+"""A worker behind the scheduler: batches that orloj_sched_decide picks are run on the
+GPU by a small text model, and their measured times go back into the histograms.
+
+The model is a stand-in of random weights (two layers unless asked otherwise) whose
+work depends on what the scheduler put together, as a served model's does: every
+application (class) has a low-rank adapter beside the shared query-key-value
+projection and its own lengths of prompt and answer, and the members of a batch keep
+their keys and values on the pages of one 8-bit cache.  A batch runs until its longest
+member has answered (§4.2.1: a batch runs as long as its slowest member):
+
+  decide      one scoring round of the runtime (§3.1: one batch at a time)
+  run         prompt step, then token steps: projection, adapters, cache write,
+              attention over the cache, projection back, next token
+  accumulate  the batch's time into the histograms of its size and classes
+              (§3.2 "Long-Term Feedback Loop"), tables rebuilt
+
+python -m paper_2209_00159_amd.stepsim prints the rounds and what they learnt.
+"""
+from __future__ import annotations
+
+import argparse
+import time
+
+import numpy as np
+import torch
+
+from . import orloj as O
+from . import worker as W
+
+
+class TextModel:
+    """Random weights and one cache per layer; requests hold pages while they run."""
+
+    def __init__(self, worker: W.Worker, applications: int, layers: int = 2, hidden: int = 1024, heads: int = 16,
+                 kv_heads: int = 4, rank: int = 16, vocab: int = 4096, pages: int = 4096, page_size: int = 16,
+                 cache_dtype: torch.dtype = torch.int8, seed: int = 0):
+        g = torch.Generator(device=worker.device)
+        g.manual_seed(seed)
+        r = lambda *s, size: (torch.randn(*s, generator=g, device=worker.device) * size).to(torch.bfloat16)  # noqa: E731
+        self.worker, self.device = worker, worker.device
+        self.heads, self.kv_heads, self.dim = heads, kv_heads, hidden // heads
+        self.embed = r(vocab, hidden, size=1.0)
+        width = (heads + 2 * kv_heads) * self.dim
+        self.layers = []
+        for _ in range(layers):
+            self.layers.append(dict(
+                qkv=r(width, hidden, size=hidden ** -0.5), out=r(hidden, heads * self.dim, size=hidden ** -0.5),
+                adapters=W.Adapters(worker, r(applications, rank, hidden, size=hidden ** -0.5),
+                                    r(applications, width, rank, size=rank ** -0.5)),
+                cache=W.Cache.empty(worker, pages, kv_heads, self.dim, page_size, cache_dtype)))
+        self.page_size = page_size
+        self.free = list(range(pages))
+
+    def place(self, lengths):
+        """Pages for requests of up to `lengths` tokens, as a table."""
+        need = [-(-n // self.page_size) for n in lengths]
+        if sum(need) > len(self.free):
+            raise RuntimeError(f"{sum(need)} pages are needed, {len(self.free)} are free")
+        table = np.full((len(lengths), max(need)), -1, np.int32)
+        for i, n in enumerate(need):
+            table[i, :n] = [self.free.pop() for _ in range(n)]
+        return table
+
+    def release(self, table):
+        self.free.extend(int(p) for p in table.ravel() if p >= 0)
+
+    def step(self, tokens: torch.Tensor, adapter: torch.Tensor, batch: W.Batch, last: torch.Tensor) -> torch.Tensor:
+        """One step over the batch's rows (token ids and adapters, int32): the logits of
+        the rows `last`."""
+        norm = lambda x: torch.nn.functional.rms_norm(x, (x.shape[-1],))  # noqa: E731
+        x = self.embed[tokens.long()]
+        hq, hk = self.heads, self.kv_heads
+        for layer in self.layers:
+            h = norm(x)
+            qkv = h @ layer["qkv"].T
+            layer["adapters"].apply(h, adapter, base=qkv, out=qkv)
+            q, k, v = qkv.unflatten(1, (hq + 2 * hk, self.dim)).split([hq, hk, hk], 1)
+            layer["cache"].write(batch, k, v)
+            x = x + layer["cache"].attend(batch, q).flatten(1) @ layer["out"].T
+        return norm(x[last.long()]) @ self.embed.T
+
+
+def run_batch(model: TextModel, classes, prompts, answers):
+    """Run one batch: requests of the given classes with their prompts (lists of token ids)
+    and numbers of tokens to answer with.  Returns (answers, milliseconds); a member that has
+    answered leaves the batch's later steps."""
+    dev = model.device
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)  # noqa: E731
+    t0 = time.perf_counter()
+    table = model.place([len(p) + n for p, n in zip(prompts, answers)])
+    lengths = [len(p) for p in prompts]
+    rows, live = list(prompts), list(range(len(prompts)))
+    said = [[] for _ in prompts]
+    pages = torch.from_numpy(table).to(dev)
+    fresh = None                    # the last step's tokens, on the device
+    while live:
+        counts = [len(rows[i]) for i in live]
+        off = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        batch = W.Batch(ints(off), ints([lengths[i] for i in live]), pages[live].contiguous(), n_rows=int(off[-1]),
+                        max_rows=max(counts), max_length=max(lengths[i] for i in live))
+        tokens = ints([t for i in live for t in rows[i]]) if fresh is None else fresh
+        adapter = ints(np.repeat([classes[i] for i in live], counts))
+        fresh = model.step(tokens, adapter, batch, ints(off[1:] - 1)).argmax(-1).to(torch.int32)
+        for i, t in zip(live, fresh.tolist()):
+            said[i].append(t)
+            rows[i] = [t]
+            lengths[i] += 1
+        keep = [k for k, i in enumerate(live) if len(said[i]) < answers[i]]
+        live = [live[k] for k in keep]
+        fresh = fresh[keep]
+    model.worker.sync()
+    model.release(table)
+    return said, (time.perf_counter() - t0) * 1e3
+
+
+def serve(requests: int = 96, applications: int = 4, batch_sizes=(1, 2, 4, 8, 16), n_bins: int = 512,
+          bin_ms: float = 1.0, slo_ms: float = 150.0, seed: int = 0, log=None, **model) -> dict:
+    """Serve `requests` requests that arrive in bursts; returns what became of them and the
+    histograms' counts [1][batch sizes][applications][bins] before and after."""
+    rng = np.random.default_rng(seed)
+    ctx = O.Context()
+    worker = W.Worker(ctx)
+    text = TextModel(worker, applications, seed=seed, **model)
+    dev = ctx.device
+    bs = np.array(batch_sizes, np.int32)
+    # what is known before anything ran: a broad prior of a few samples a bin
+    prior = np.zeros((1, bs.size, applications, n_bins), np.uint32)
+    for c in range(applications):
+        prior[0, :, c, 4 + 4 * c:64 + 24 * c:4] = 1
+    counts = torch.from_numpy(prior.view(np.int32)).to(dev)
+    ccdf, support = torch.empty(counts.shape, device=dev), torch.empty(counts.shape[:-1] + (2,), dtype=torch.int32, device=dev)
+    ctx.build_cdfs(counts, ccdf, support)
+    width = torch.full((1,), bin_ms, dtype=torch.float64, device=dev)
+    grid = O.make_grid(1, applications, n_bins, bs, width)
+    sched = O.Sched(ctx, grid, ccdf, support, np.full((1, applications), 1.0), 1e-4)
+    prompt_of = lambda c: int(rng.integers(8, 64 * (c + 1)))      # noqa: E731
+    answer_of = lambda c: int(rng.geometric(1.0 / (6 * (c + 1))))  # noqa: E731
+    run_batch(text, [0], [[1, 2, 3]], [2])                         # first launches
+    now, late, on_time, dropped, admitted, rounds = 0.0, 0, 0, 0, 0, 0
+    while admitted < requests or sched.queue_length(0):
+        n = min(int(rng.integers(4, 24)), requests - admitted)
+        if n:
+            cls = rng.integers(0, applications, n)
+            sched.admit(np.zeros(n), cls, now + slo_ms * (1.0 + rng.random(n)))
+            admitted += n
+        d = sched.decide(now)
+        dropped += d["dropped"]
+        members = d["batch_class"].tolist()
+        if not members:
+            now += bin_ms
+            if not n and sched.queue_length(0) and not d["dropped"]:
+                now += slo_ms            # nothing scores: let the rest run out
+            continue
+        prompts = [rng.integers(0, text.embed.shape[0], prompt_of(c)).tolist() for c in members]
+        _, ms = run_batch(text, members, prompts, [answer_of(c) for c in members])
+        now += ms
+        rounds += 1
+        met = int(np.sum(d["batch_deadline_ms"] >= now))
+        on_time, late = on_time + met, late + len(members) - met
+        size = int(np.searchsorted(bs, int(d["sel_bs"][0])))
+        i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)  # noqa: E731
+        k = len(members)
+        O.accumulate(ctx, grid, counts, i32([0] * k), i32([size] * k), i32(members),
+                     torch.full((k,), ms, dtype=torch.float64, device=dev))
+        ctx.build_cdfs(counts, ccdf, support)
+        if log:
+            log(f"round {rounds}: {k} of batch size {bs[size]}, classes {sorted(members)}, {ms:.1f} ms, {met} in time")
+    ctx.sync()
+    return dict(rounds=rounds, on_time=on_time, late=late, dropped=dropped, prior=prior,
+                counts=counts.cpu().numpy().view(np.uint32), free_pages=len(text.free))
+
+
+def main():
+    ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
+    ap.add_argument("--requests", type=int, default=96)
+    ap.add_argument("--applications", type=int, default=4)
+    ap.add_argument("--layers", type=int, default=2)
+    ap.add_argument("--fp8", action="store_true", help="cache in e4m3 instead of 8-bit integers")
+    ap.add_argument("--seed", type=int, default=0)
+    a = ap.parse_args()
+    out = serve(a.requests, a.applications, layers=a.layers, seed=a.seed, log=print,
+                cache_dtype=torch.float8_e4m3fn if a.fp8 else torch.int8)
+    new = out["counts"].astype(np.int64) - out["prior"]
+    for c in range(a.applications):
+        k = new[0, :, c].sum(0)
+        if k.sum():
+            print(f"class {c}: {k.sum()} samples, mean {np.average(np.arange(k.size) + 0.5, weights=k):.1f} ms")
+    print(f"{out['rounds']} batches: {out['on_time']} requests in time, {out['late']} late, {out['dropped']} dropped")
+
+
+if __name__ == "__main__":
+    main()

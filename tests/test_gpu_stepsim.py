@@ -1,0 +1,76 @@
+"""The worker's operators together, behind the scheduler (stepsim)."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2209_00159_amd import stepsim as S
+from paper_2209_00159_amd import worker as W
+
+pytestmark = pytest.mark.gpu
+
+
+def plain_logits(model, layer_inputs, tokens, cls):
+    """One request's logits of its last token, all of its tokens in one pass in 64 bits, keys and
+    values as the cache holds them (rounded to its codes)."""
+    norm = lambda x: x / torch.sqrt((x * x).mean(-1, keepdim=True) + torch.finfo(torch.bfloat16).eps)  # noqa: E731
+    x = model.embed.cpu().double()[tokens]
+    hq, hk, D = model.heads, model.kv_heads, model.dim
+    n = len(tokens)
+    for layer in model.layers:
+        h = norm(x)
+        down, up = (t.cpu().double() for t in layer["adapters"]._keep[:2])
+        qkv = h @ layer["qkv"].cpu().double().T + (h @ down[cls].T) @ up[cls].T
+        q, k, v = qkv.unflatten(1, (hq + 2 * hk, D)).split([hq, hk, hk], 1)
+
+        def cached(t):
+            scale = t.abs().amax(-1, keepdim=True) / 127.0
+            return torch.round(t / scale) * scale
+        k, v = (cached(t).repeat_interleave(hq // hk, 1) for t in (k, v))
+        s = torch.einsum("ihd,jhd->hij", q, k) * D ** -0.5
+        s = s.masked_fill(torch.ones(n, n, dtype=torch.bool).triu(1), -torch.inf)
+        x = x + torch.einsum("hij,jhd->ihd", torch.softmax(s, -1), v).flatten(1) @ layer["out"].cpu().double().T
+    return norm(x[-1]) @ model.embed.cpu().double().T
+
+
+def test_steps_of_a_batch_against_one_request_at_a_time():
+    """Prompts and token steps of a mixed batch, through pages, against each request by itself and
+    whole.  16-bit activations and 8-bit keys and values leave about a percent of the logits' size;
+    a wrong row, page, adapter or mask leaves all of it."""
+    print("stepsim: steps", flush=True)
+    worker = W.Worker()
+    model = S.TextModel(worker, 3, layers=2, hidden=256, heads=8, kv_heads=2, rank=8, vocab=512, pages=64, seed=1)
+    g = np.random.default_rng(3)
+    classes = [2, 0, 1, 2]
+    prompts = [g.integers(0, 512, n).tolist() for n in (5, 33, 1, 16)]
+    table = model.place([len(p) + 3 for p in prompts])
+    dev = worker.device
+    i = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)  # noqa: E731
+    seen = [list(p) for p in prompts]
+    rows = [list(p) for p in prompts]
+    for _ in range(3):
+        counts = [len(r) for r in rows]
+        off = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        batch = W.Batch(i(off), i([len(s) for s in seen]), torch.from_numpy(table).to(dev))
+        logits = model.step(i(sum(rows, [])), i(np.repeat(classes, counts)), batch, i(off[1:] - 1))
+        worker.sync()
+        for r in range(4):
+            want = plain_logits(model, None, seen[r], classes[r])
+            got = logits[r].cpu().double()
+            assert float((got - want).norm() / want.norm()) < 0.05, r
+        for r, t in enumerate(logits.argmax(-1).tolist()):
+            seen[r].append(t)
+            rows[r] = [t]
+    model.release(table)
+    assert len(model.free) == 64
+
+
+@pytest.mark.parametrize("dtype", [torch.int8, torch.float8_e4m3fn])
+def test_serving(dtype):
+    """Every request ends in time, late or dropped; every batch's time lands in the histograms; no
+    page is lost."""
+    print("stepsim: serve", dtype, flush=True)
+    out = S.serve(40, 3, layers=1, hidden=256, heads=8, kv_heads=2, rank=8, vocab=512, pages=1024, seed=2,
+                  cache_dtype=dtype)
+    assert out["on_time"] + out["late"] + out["dropped"] == 40
+    assert out["rounds"] > 0 and out["free_pages"] == 1024
+    assert int(out["counts"].sum()) - int(out["prior"].sum()) == out["on_time"] + out["late"]

@@ -241,6 +241,26 @@ def test_cache_of_many_requests(worker):
     worker.sync()
 
 
+def test_pages_past_32_bits(worker):
+    """Pages more than 2^32 bytes into the cache hold what near ones do."""
+    say("pages past 32 bits")
+    far = W.Cache.empty(worker, 8300, 8, 256, 256, torch.int8)      # 512 KiB a page
+    near = W.Cache.empty(worker, 4, 8, 256, 256, torch.int8)
+    i = lambda v: torch.tensor(v, dtype=torch.int32, device=worker.device)  # noqa: E731
+    assert far.k.numel() > 2 ** 32
+    g = torch.Generator().manual_seed(1)
+    k, v, q = (torch.randn(300, h, 256, generator=g).to(torch.bfloat16).to(worker.device) for h in (8, 8, 16))
+    got = []
+    for cache, pages in ((far, [8299, 8230]), (near, [1, 3])):
+        batch = W.Batch(i([0, 300]), i([300]), i([pages]))
+        cache.write(batch, k, v)
+        one = W.Batch(i([0, 1]), i([300]), i([pages]))
+        got.append([*cache.read(batch, dtype=torch.float32), cache.attend(batch, q), cache.attend(one, q[:1])])
+    worker.sync()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
 # -- attention -----------------------------------------------------------------------
 def check_attend(worker, p, q, scale=None, tree=None, layout=None):
     dev = q.to(worker.device)
@@ -641,6 +661,7 @@ def test_refusals(worker):
     refused(O.ORLOJ_E_INVALID, lambda: c.attend(b, z(2, 2, 64), scale=math.inf))
     refused(O.ORLOJ_E_UNSUPPORTED, lambda: c.attend(batch_of(65, 65), z(65, 2, 64), tree=z(65, dtype=torch.int64)))
     refused(O.ORLOJ_E_INVALID, lambda: c.attend(batch_of(n_rows=2, max_rows=-1, max_length=4), z(2, 2, 64)))
+    refused(O.ORLOJ_E_UNSUPPORTED, lambda: c.read(batch_of(n_rows=2, max_rows=2, max_length=(1 << 30) + 1)))
     for bad in (lambda: W.Cache(worker, c.k, c.v, c.k_scale, c.v_scale, 65),
                 lambda: W.Cache(worker, c.k, c.v, c.k_scale[:2], c.v_scale, 64),
                 lambda: c.write(b, z(2, 2, 63), z(2, 2, 64)), lambda: c.write(b, z(3, 2, 64), z(2, 2, 64)),
