@@ -1076,12 +1076,12 @@ struct Tile {
 // The order of the k index is free as long as both operands agree, so no operand
 // goes through LDS: a lane loads its share of the page rows whole (16 bytes of K,
 // DP / 16 of V a token) and the codes become 16-bit floats in registers.
-// Four waves take every fourth tile, the next one's loads in flight; their sums meet
-// in LDS.
+// Four waves take every fourth tile, the next one's loads in flight (the first's while
+// the queries are prepared); their sums meet in LDS.
 template <int FMT, int DP, int NT>
 __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend_kernel(AttendArgs a) {
     constexpr int R = 16 * NT, ND = DP / 64, MT = DP / 16;
-    __shared__ __attribute__((aligned(16))) float o_sum[R][DP + 4];
+    __shared__ __attribute__((aligned(16))) float o_of[kWaves][R][DP + 4];
     __shared__ float c_of[kWaves][R], l_of[kWaves][R];
     const CacheArgs& c = a.c;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -1090,7 +1090,6 @@ __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend
     Part w;
     if (!part_of(a, r, block, split, w)) return;
     Pairs<DP, NT> q;
-    start<DP, NT>(a, w, head, w.pair0, q);
 
     const int tiles = (w.stop - w.begin + 31) >> 5;
     const int last_part = (w.end - 1) >> 4;   // 16-token parts beyond it hold nothing
@@ -1156,9 +1155,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend
     };
 
     const int mine = tiles > wave ? (tiles - wave + kWaves - 1) / kWaves : 0;
+    Tile<DP> x, y;
+    if (mine > 0) load(0, x);
+    start<DP, NT>(a, w, head, w.pair0, q);    // while the first tile is on its way
     if (mine > 0) {
-        Tile<DP> x, y;
-        load(0, x);
         int it = 0;
         for (; it + 2 <= mine; it += 2) {
             load(it + 1, y);
@@ -1169,7 +1169,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend
         if (it < mine) use(it, x);
     }
 
-    // the four waves' sums, in turn, so that the order of the additions is fixed
+    // the four waves' sums, added in their order
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         q.l[t] = column_sum(q.l[t]);
@@ -1177,40 +1177,26 @@ __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend
             c_of[wave][16 * t + n] = q.ref[t];
             l_of[wave][16 * t + n] = q.l[t];
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < MT; j += 4)
+                *(float4_t*)&o_of[wave][16 * t + n][(4 * g + i) * MT + j] =
+                    float4_t{q.o[t][j][i], q.o[t][j + 1][i], q.o[t][j + 2][i], q.o[t][j + 3][i]};
     }
     __syncthreads();
-    float by[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int k = 16 * t + n;
-        by[t] = __builtin_amdgcn_exp2f(fminf(fminf(c_of[0][k], c_of[1][k]), fminf(c_of[2][k], c_of[3][k])) - q.ref[t]);
-    }
-    for (int v = 0; v < kWaves; ++v) {
-        if (v == wave) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float* at = &o_sum[16 * t + n][(4 * g + i) * MT];
-#pragma unroll
-                    for (int j = 0; j < MT; j += 4) {
-                        float4_t x = {q.o[t][j][i], q.o[t][j + 1][i], q.o[t][j + 2][i], q.o[t][j + 3][i]};
-                        x *= by[t];
-                        *(float4_t*)(at + j) = v ? *(float4_t*)(at + j) + x : x;
-                    }
-                }
-        }
-        __syncthreads();
-    }
     for (int k = threadIdx.x; k < R * (DP / 8); k += kThreads) {
         const int row = k / (DP / 8), d = k % (DP / 8) * 8;
         if (w.pair0 + row >= w.pairs) break;
         const float ref = fminf(fminf(c_of[0][row], c_of[1][row]), fminf(c_of[2][row], c_of[3][row]));
-        float sum = 0.0f, z[8];
+        float sum = 0.0f, z[8] = {};
 #pragma unroll
-        for (int v = 0; v < kWaves; ++v) sum += l_of[v][row] * __builtin_amdgcn_exp2f(ref - c_of[v][row]);
+        for (int v = 0; v < kWaves; ++v) {
+            const float by = __builtin_amdgcn_exp2f(ref - c_of[v][row]);
+            sum += l_of[v][row] * by;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = o_sum[row][d + j];
+            for (int j = 0; j < 8; ++j) z[j] = fmaf(o_of[v][row][d + j], by, z[j]);
+        }
         put_out<DP>(a, w, split, head, w.pair0 + row, d, z, sum, ref);
     }
 }
