@@ -593,8 +593,8 @@ typedef struct orloj_cache {
  * The requests of a batch, their new tokens' rows stored back to back.  Request
  * r has d_length[r] tokens, its rows d_row_off[r] .. d_row_off[r+1]-1 being the
  * last of them.  Everything is device memory, so that a captured step can be
- * replayed with other lengths; max_rows and max_length bound them on the host
- * (they size launches).  Data errors: offsets that decrease or leave
+ * replayed with other lengths; max_rows and max_length (at most 2^30) bound them on
+ * the host (they size launches).  Data errors: offsets that decrease or leave
  * [0, n_rows], more rows than max_rows or than the length, a length beyond max_length
  * or beyond the table, a needed page outside [0, n_pages).  Entries of the
  * table past a request's last page are not read.
@@ -645,9 +645,10 @@ int orloj_worker_cache_read(orloj_worker *worker, const orloj_cache *cache,
  * hold; one it sees with a NaN key or value makes it NaN.
  * dtype (ORLOJ_F16 or ORLOJ_BF16) is the type of q and out.  The scores' sums,
  * the softmax's statistics and the output's sums are held in 32 bits; q, scaled
- * per row, and the weights enter the products in 16-bit floating point with 11
- * significant bits, the codes exactly; value scales up to 2^100 (values up to
- * 2^106) leave the weights in that format's range.  Results are the same bits every time
+ * per row, enters the products in 16-bit floating point with 11 significant
+ * bits, the weights likewise (in two such parts where the output is float16),
+ * the codes exactly; value scales up to 2^100 (values up to 2^106) leave the
+ * weights in that format's range.  Results are the same bits every time
  * for the same arguments.
  */
 int orloj_worker_attend(orloj_worker *worker, const orloj_cache *cache, const orloj_batch *batch,

@@ -938,11 +938,14 @@ __device__ __forceinline__ int largest_bits(const float4_t (&v)[2]) {
 }
 
 // Products of column t with 32 tokens from t0 on -> their weights times the value
-// scales, as the operand of the product with V.  all: every row sees all of them;
-// vmax: largest_bits(vs).
-template <int DP, int NT>
+// scales, as the operand of the product with V, and with FINE what that leaves of them.
+// all: every row sees all of them; vmax: largest_bits(vs).
+// One 16-bit part rounds a weight to 11 bits, which the sum's own rounding to bfloat16
+// (8 bits) hides; beside a float16 output (11 bits) it would be half the error, so those
+// take two parts and a second product.
+template <bool FINE, int DP, int NT>
 __device__ __forceinline__ half8_t weigh(const Part& w, Pairs<DP, NT>& x, int t, const float4_t (&s)[2], const float4_t (&ks)[2],
-                                         const float4_t (&vs)[2], int vmax, int t0, bool all) {
+                                         const float4_t (&vs)[2], int vmax, int t0, bool all, half8_t& rest) {
     const int g = threadIdx.x >> 4 & 3;
     float u[8], v[8], mx = -INFINITY;
 #pragma unroll
@@ -988,6 +991,7 @@ __device__ __forceinline__ half8_t weigh(const Part& w, Pairs<DP, NT>& x, int t,
         const float e = __builtin_amdgcn_exp2f(fmaf(u[j], x.f[t], x.ref[t]));
         x.l[t] += e;
         p[j] = (_Float16)(e * v[j]);
+        if (FINE) rest[j] = (_Float16)fmaf(e, v[j], -(float)p[j]);
     }
     return p;
 }
@@ -1078,7 +1082,7 @@ struct Tile {
 // DP / 16 of V a token) and the codes become 16-bit floats in registers.
 // Four waves take every fourth tile, the next one's loads in flight (the first's while
 // the queries are prepared); their sums meet in LDS.
-template <int FMT, int DP, int NT>
+template <int FMT, bool FINE, int DP, int NT>
 __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend_kernel(AttendArgs a) {
     constexpr int R = 16 * NT, ND = DP / 64, MT = DP / 16;
     __shared__ __attribute__((aligned(16))) float o_of[kWaves][R][DP + 4];
@@ -1136,9 +1140,9 @@ __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend
         }
         const bool all = t0 + 32 <= min(w.plain, w.stop);
         const int vmax = largest_bits(x.vs);
-        half8_t p[NT];
+        half8_t p[NT], rest[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) p[t] = weigh<DP, NT>(w, q, t, s[t], x.ks, x.vs, vmax, t0, all);
+        for (int t = 0; t < NT; ++t) p[t] = weigh<FINE, DP, NT>(w, q, t, s[t], x.ks, x.vs, vmax, t0, all, rest[t]);
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
             uint32_t words[8];
@@ -1149,8 +1153,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                for (int t = 0; t < NT; ++t) {
                     q.o[t][4 * d + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[b], p[t], q.o[t][4 * d + b], 0, 0, 0);
+                    if (FINE) q.o[t][4 * d + b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[b], rest[t], q.o[t][4 * d + b], 0, 0, 0);
+                }
         }
     };
 
@@ -1207,7 +1213,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend
 // ahead of the products; the codes of the two tiles after it are in flight.  Where a workgroup's
 // pairs need half its waves or fewer, the others take every second 32 tokens of them, and
 // the two sums are joined at the end.
-template <int FMT, int DP, int NT, int WAVES>
+template <int FMT, bool FINE, int DP, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attend_rows_kernel(AttendArgs a) {
     constexpr int ND = DP / 64, MT = DP / 16, TK = 64, PARTS = TK / 16;
     constexpr int KU = PARTS * ND, VU = PARTS / 2 * ND;   // 16-byte pieces of K, words of V for 32 tokens
@@ -1326,14 +1332,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_rows_kernel(AttendArgs a
                     vs[i] = *(const float4_t*)&scale[b][1][32 * h + 16 * i + 4 * g];
                 }
                 const int vmax = largest_bits(vs);
-                half8_t p[NT];
+                half8_t p[NT], rest[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) p[t] = weigh<DP, NT>(w, q, t, s[t], ks, vs, vmax, t0 + 32 * h, all);
+                for (int t = 0; t < NT; ++t) p[t] = weigh<FINE, DP, NT>(w, q, t, s[t], ks, vs, vmax, t0 + 32 * h, all, rest[t]);
 #pragma unroll
                 for (int j = 0; j < MT; ++j) {
                     const half8_t v = vs_[b][h][j][lane];
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) q.o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[t], q.o[t][j], 0, 0, 0);
+                    for (int t = 0; t < NT; ++t) {
+                        q.o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[t], q.o[t][j], 0, 0, 0);
+                        if (FINE) q.o[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, rest[t], q.o[t][j], 0, 0, 0);
+                    }
                 }
             }
         }
@@ -1653,27 +1662,27 @@ int attend_blocks(orloj_worker* w, AttendArgs& a, const char* what, void (*kerne
                   dim3(a.c.max_rows, (a.q_heads + kWaves - 1) / kWaves, a.c.requests), kThreads, a);
 }
 
-template <int FMT, int DP>
+template <int FMT, bool FINE, int DP>
 int attend_dim(orloj_worker* w, AttendArgs& a) {
     const int64_t pairs = (int64_t)a.c.max_rows * a.group;
-    if (pairs <= 16) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, DP, 1>, kThreads, 16, 2);
+    if (pairs <= 16) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, FINE, DP, 1>, kThreads, 16, 2);
     // beyond 128 dimensions the registers hold the sums of 16 pairs a wave
     if constexpr (DP <= 128) {
-        if (pairs <= 32) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, DP, 2>, kThreads, 32, 2);
-        if (pairs > 128) return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, DP, 2, 8>, 512, 256, 2);
-        return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, DP, 2, 4>, kThreads, 128, 2);
+        if (pairs <= 32) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, FINE, DP, 2>, kThreads, 32, 2);
+        if (pairs > 128) return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, FINE, DP, 2, 8>, 512, 256, 2);
+        return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, FINE, DP, 2, 4>, kThreads, 128, 2);
     } else {
-        return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, DP, 1, 8>, 512, 128, 2);
+        return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, FINE, DP, 1, 8>, 512, 128, 2);
     }
 }
 
-template <int FMT>
+template <int FMT, bool FINE>
 int attend(orloj_worker* w, AttendArgs& a) {
     switch (a.c.pad) {
-        case 64: return attend_dim<FMT, 64>(w, a);
-        case 128: return attend_dim<FMT, 128>(w, a);
-        case 192: return attend_dim<FMT, 192>(w, a);
-        default: return attend_dim<FMT, 256>(w, a);
+        case 64: return attend_dim<FMT, FINE, 64>(w, a);
+        case 128: return attend_dim<FMT, FINE, 128>(w, a);
+        case 192: return attend_dim<FMT, FINE, 192>(w, a);
+        default: return attend_dim<FMT, FINE, 256>(w, a);
     }
 }
 
@@ -1798,7 +1807,9 @@ int orloj_worker_attend(orloj_worker* w, const orloj_cache* cache, const orloj_b
     a.q_heads = n_q_heads;
     a.group = n_q_heads / a.c.heads;
     a.half = dtype == ORLOJ_F16;
-    return a.c.format == ORLOJ_CACHE_INT8 ? attend<ORLOJ_CACHE_INT8>(w, a) : attend<ORLOJ_CACHE_FP8>(w, a);
+    if (a.c.format == ORLOJ_CACHE_INT8)
+        return a.half ? attend<ORLOJ_CACHE_INT8, true>(w, a) : attend<ORLOJ_CACHE_INT8, false>(w, a);
+    return a.half ? attend<ORLOJ_CACHE_FP8, true>(w, a) : attend<ORLOJ_CACHE_FP8, false>(w, a);
 }
 
 }  // extern "C"
