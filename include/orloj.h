@@ -543,7 +543,7 @@ enum orloj_dtype { ORLOJ_F32 = 0, ORLOJ_F16 = 1, ORLOJ_BF16 = 2 };
  * d_base may be d_y (with the same stride), no other overlap.  h, the sums and
  * the addition are held in 32 bits or more; y is rounded once.  Rows of one
  * adapter need not be adjacent, though weights are read once per 16
- * adjacent rows that share them (64 in calls of more than 256 rows).
+ * adjacent rows that share them (64 in calls of more than 1024 rows).
  *
  * dtype (ORLOJ_F16 or ORLOJ_BF16) is the type of d_x, d_base, d_y and the
  * weights.  Strides are in elements between rows, at least d_in (x) or d_out

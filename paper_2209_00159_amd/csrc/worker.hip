@@ -137,6 +137,10 @@ __device__ __forceinline__ ushort8_t cut_piece(ushort8_t v, int at, int start, i
 // v_mfma_f32_16x16x32.  Both operands are contiguous along k, so a lane loads its
 // 16 bytes of each straight into the operand's registers, 64 adjacent bytes a row.  The four waves take 64 of each 256 elements; their sums meet in LDS,
 // those of the splits of d_in in adapt_up_kernel.
+// Measured: 8192 rows of 4096 at rank 64, 46 us for 64 MiB of rows (a copy's rate would
+// take 13 us).  Left out in turn, the weights' loads took 17 us of it, the rows' 19, the
+// join 5: neighbouring lanes of an operand are different rows, which the load path
+// takes one by one.  64 rows of 32 adapters, rank 16: 5.5 us, the chain of its loads.
 // The rows' distinct adapters: with NT = 1 (few rows) the z-th of the grid's z-th
 // workgroup, else one after the other (rows of a prompt share theirs).
 template <class E, int RT, int NT>
@@ -377,7 +381,8 @@ __device__ __forceinline__ void put_y(const AdaptArgs& a, int64_t t, int o0, con
 //
 // Few rows: 16 a workgroup and 64 outputs, every fourth distinct adapter a wave.  What
 // costs is the chain of loads, so those that do not wait for h go first: the bases and
-// the weights of the wave's first PRE adapters.
+// the weights of the wave's first PRE adapters (4096 outputs, 64 rows of 32 adapters at
+// rank 16: 7 us, 10 before).
 template <class E, int STEPS, bool FULL>
 __device__ __forceinline__ void up_few(const AdaptArgs& a, int o0) {
     constexpr int PITCH = 32 * STEPS + 8, PRE = 4 / STEPS;
@@ -444,7 +449,11 @@ __global__ __launch_bounds__(kThreads) void adapt_up_few_kernel(AdaptArgs a) {
 }
 
 // Many rows: 64 a workgroup, 64 outputs a wave of each block of 256; the rows' distinct
-// adapters (adjacent rows of a prompt share theirs) one after the other.
+// adapters (adjacent rows of a prompt share theirs) one after the other.  Two blocks a
+// workgroup where there are enough of them (106 us for both kernels at 8192 rows, 4096
+// wide, rank 64; one block 114, four 108).
+// Measured there: 50 us for 128 MiB of base and y; without its products it took 28 us,
+// the rate of a copy.
 template <class E, int STEPS, int NT>
 __global__ __launch_bounds__(kThreads) void adapt_up_kernel(AdaptArgs a) {
     constexpr int PITCH = 32 * STEPS + 8, ROWS = 16 * NT;
@@ -658,7 +667,9 @@ __device__ __forceinline__ void store_elements(typename E::T* p, int count, cons
     }
 }
 
-// Bound by its bytes: 2 D in and D + 4 out a vector (16-bit activations).
+// Bound by its bytes, D + 4 out for 2 D in a vector of 16-bit activations: 16384 rows of
+// 2 x 8 heads x 128 (bf16 to fp8) take 22.6 us, 4.5 TB/s; read back in 19.4 us, 5.2 TB/s,
+// a copy's rate.  With a vector's 16 lanes each looking its row up: 59 and 39 us.
 template <class E, int FMT, int ND>
 __global__ __launch_bounds__(kThreads) void cache_write_kernel(CopyArgs a) {
     constexpr int N = 4 * ND, ROUNDS = kVectors / 4;
@@ -1082,6 +1093,10 @@ struct Tile {
 // DP / 16 of V a token) and the codes become 16-bit floats in registers.
 // Four waves take every fourth tile, the next one's loads in flight (the first's while
 // the queries are prepared); their sums meet in LDS.
+// Bound by the cache's bytes: four requests of 65536 to 131072 tokens (8 heads x 128, 8
+// query heads each, fp8) in 153 us, 5.5 TB/s; 64 of 64 to 8192 tokens in 130 us, where the
+// longest is what is waited for (64 of 8000 to 8192: 5.7 TB/s).  Two waves a SIMD: with
+// one, 187 us; with three the registers spill (400 us).
 template <int FMT, bool FINE, int DP, int NT>
 __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend_kernel(AttendArgs a) {
     constexpr int R = 16 * NT, ND = DP / 64, MT = DP / 16;
@@ -1213,6 +1228,12 @@ __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend
 // ahead of the products; the codes of the two tiles after it are in flight.  Where a workgroup's
 // pairs need half its waves or fewer, the others take every second 32 tokens of them, and
 // the two sums are joined at the end.
+// Bound by the vector instructions beside the products (a wave's tile of 64 tokens: 64
+// products of 16 cycles, about 400 instructions): chunks of four prompts of up to 2048
+// rows after up to 4096 tokens, 32 query heads over 8 x 128, in 346 us, 0.63 PFLOP/s of
+// visible pairs.  Eight waves a tile against four: 359 and 368 us when they were
+// compared; the codes of two tiles in flight against one: 346 and 351 us; trees 119
+// and 127 us.
 template <int FMT, bool FINE, int DP, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attend_rows_kernel(AttendArgs a) {
     constexpr int ND = DP / 64, MT = DP / 16, TK = 64, PARTS = TK / 16;
@@ -1537,9 +1558,10 @@ int adapt_tiles(orloj_worker* w, AdaptArgs& a) {
 
 template <class E>
 int adapt(orloj_worker* w, AdaptArgs& a) {
-    // few rows: 16 a workgroup, their adapters side by side; many: 64, one adapter after
-    // the other
-    if (a.rows <= 256) {
+    // few rows: 16 a workgroup, their adapters side by side; many: 64, one adapter after the
+    // other.  At 4096 wide and rank 64, us few / many: 256 rows of 32 adapters 44 / 236, 1024
+    // 140 / 249; 256 rows of 8 prompts 18 / 44, 1024 43 / 38, 2048 62 / 40
+    if (a.rows <= 1024) {
         if (a.rank <= 16) return adapt_tiles<E, 1, 1>(w, a);
         if (a.rank <= 32) return adapt_tiles<E, 2, 1>(w, a);
         if (a.rank <= 64) return adapt_tiles<E, 4, 1>(w, a);
@@ -1640,7 +1662,9 @@ int attend_blocks(orloj_worker* w, AttendArgs& a, const char* what, void (*kerne
     a.block_pairs = block_pairs;
     const int64_t groups = (int64_t)a.c.requests * a.c.heads * blocks;
     // per_unit workgroups a unit where there are fewer, from at least 256 tokens each:
-    // as many as a unit holds at once
+    // the two that a unit holds at once.  More even out requests of different lengths but
+    // begin, end and join more often: 3, 4, 6 or 8 a unit against 2, with 4 to 128
+    // requests of 64 to 8192 tokens, took 0.9 to 1.4 times as long
     const int64_t want = (per_unit * (int64_t)w->ctx->n_cu + groups - 1) / groups;
     const int64_t most = std::max<int64_t>(1, (a.c.max_length + 255) / 256);
     const int64_t parts = std::min(want, most);
@@ -1665,6 +1689,9 @@ int attend_blocks(orloj_worker* w, AttendArgs& a, const char* what, void (*kerne
 template <int FMT, bool FINE, int DP>
 int attend_dim(orloj_worker* w, AttendArgs& a) {
     const int64_t pairs = (int64_t)a.c.max_rows * a.group;
+    // up to 32 pairs a wave each takes all of them (64 requests of up to 8192 tokens, 32
+    // pairs: 151 us, 224 us in attend_rows_kernel); up to 128 four waves leave two workgroups
+    // a unit (16 requests of 96 pairs: 97 us, 117 us with eight; but 64 of 80: 332 and 297)
     if (pairs <= 16) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, FINE, DP, 1>, kThreads, 16, 2);
     // beyond 128 dimensions the registers hold the sums of 16 pairs a wave
     if constexpr (DP <= 128) {

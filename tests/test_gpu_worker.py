@@ -81,6 +81,11 @@ def check_adapt(worker, d, use_base=True, use_scale=True):
     (128, 4, 256, 128, 128, 0, True),
     (130, 3, 2048, 96, 33, 0, False),
     (700, 6, 512, 640, 24, 0, True),
+    (1025, 4, 7, 5, 3, 0, True),
+    (1030, 5, 333, 517, 12, 3, True),
+    (1100, 6, 512, 640, 24, 0, True),
+    (1100, 3, 1032, 96, 33, 8, False),
+    (1200, 4, 256, 136, 128, 0, True),
 ])
 def test_adapters(worker, dtype, rows, n, d_in, d_out, rank, pad, ragged):
     say("adapt", dtype, rows, n, d_in, d_out, rank, pad, ragged)
@@ -89,12 +94,12 @@ def test_adapters(worker, dtype, rows, n, d_in, d_out, rank, pad, ragged):
     check_adapt(worker, d, use_base=False, use_scale=False)
 
 
+@pytest.mark.parametrize("rows", [150, 1150])
 @pytest.mark.parametrize("ids", ["one", "none", "pairs", "blocks"])
-def test_adapters_of_adjacent_rows(worker, ids):
-    say("adapt ids", ids)
-    rows = 150
+def test_adapters_of_adjacent_rows(worker, ids, rows):
+    say("adapt ids", ids, rows)
     i = torch.arange(rows)
-    pick = dict(one=i * 0 + 2, none=i * 0 - 1, pairs=i // 2 % 5, blocks=i // 40)[ids]
+    pick = dict(one=i * 0 + 2, none=i * 0 - 1, pairs=i // 2 % 5, blocks=i // 40 % 5)[ids]
     d = adapt_inputs(5, rows, 5, 256, 384, 16, torch.bfloat16, none=0.0, ids=pick)
     got = check_adapt(worker, d)
     if ids == "none":
