@@ -594,7 +594,8 @@ typedef struct orloj_cache {
  * r has d_length[r] tokens, its rows d_row_off[r] .. d_row_off[r+1]-1 being the
  * last of them.  Everything is device memory, so that a captured step can be
  * replayed with other lengths; max_rows and max_length (at most 2^30) bound them on
- * the host (they size launches).  Data errors: offsets that decrease or leave
+ * the host (they size launches; ORLOJ_E_INVALID where n_rows > n_requests max_rows).
+ * Data errors: offsets that decrease or leave
  * [0, n_rows], more rows than max_rows or than the length, a length beyond max_length
  * or beyond the table, a needed page outside [0, n_pages).  Entries of the
  * table past a request's last page are not read.

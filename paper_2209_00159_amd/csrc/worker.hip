@@ -870,6 +870,12 @@ struct Part {
     int begin, stop;            // its split's
 };
 
+// The workgroup's split: turned by head and request, since workgroups go to the eight XCDs
+// in turn and a number of splits that shares a factor with eight would else give an XCD the
+// same ones of all requests, the last of which short requests do not have (trees of 16
+// requests of 64 to 8192 tokens in 16 splits: 113 us, 79 us in 12).
+__device__ __forceinline__ int split_of_group() { return (blockIdx.x + blockIdx.y + blockIdx.z) % gridDim.x; }
+
 __device__ __forceinline__ bool part_of(const AttendArgs& a, int r, int block, int split, Part& w) {
     if (!request_of(a.c, r, w.first, w.rows, w.length)) return false;
     w.pair0 = block * a.block_pairs;
@@ -1094,9 +1100,9 @@ struct Tile {
 // Four waves take every fourth tile, the next one's loads in flight (the first's while
 // the queries are prepared); their sums meet in LDS.
 // Bound by the cache's bytes: four requests of 65536 to 131072 tokens (8 heads x 128, 8
-// query heads each, fp8) in 153 us, 5.5 TB/s; 64 of 64 to 8192 tokens in 130 us, where the
-// longest is what is waited for (64 of 8000 to 8192: 5.7 TB/s).  Two waves a SIMD: with
-// one, 187 us; with three the registers spill (400 us).
+// query heads each, fp8) in 153 us, 5.5 TB/s; 64 of 64 to 8192 tokens with the join in
+// 106 us, 4.7 TB/s.  Two waves a SIMD: when the latter took 138 us, one wave took 186 and
+// three, whose registers spill, 400.
 template <int FMT, bool FINE, int DP, int NT>
 __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend_kernel(AttendArgs a) {
     constexpr int R = 16 * NT, ND = DP / 64, MT = DP / 16;
@@ -1105,7 +1111,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend
     const CacheArgs& c = a.c;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int split = blockIdx.x, head = blockIdx.y % c.heads, block = blockIdx.y / c.heads, r = blockIdx.z;
+    const int split = split_of_group(), head = blockIdx.y % c.heads, block = blockIdx.y / c.heads, r = blockIdx.z;
     Part w;
     if (!part_of(a, r, block, split, w)) return;
     Pairs<DP, NT> q;
@@ -1230,10 +1236,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 && NT == 1 ? 2 : 1) void attend
 // the two sums are joined at the end.
 // Bound by the vector instructions beside the products (a wave's tile of 64 tokens: 64
 // products of 16 cycles, about 400 instructions): chunks of four prompts of up to 2048
-// rows after up to 4096 tokens, 32 query heads over 8 x 128, in 346 us, 0.63 PFLOP/s of
-// visible pairs.  Eight waves a tile against four: 359 and 368 us when they were
-// compared; the codes of two tiles in flight against one: 346 and 351 us; trees 119
-// and 127 us.
+// rows after up to 4096 tokens, 32 query heads over 8 x 128, in 347 us, 0.62 PFLOP/s of
+// visible pairs; trees of 16 requests of up to 24 tokens after up to 12000 in 82 us.
+// Compared on the chunks: eight waves a tile against four 359 and 368 us, the codes of
+// two tiles in flight against one 346 and 351.
 template <int FMT, bool FINE, int DP, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attend_rows_kernel(AttendArgs a) {
     constexpr int ND = DP / 64, MT = DP / 16, TK = 64, PARTS = TK / 16;
@@ -1248,7 +1254,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_rows_kernel(AttendArgs a
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int blocks = gridDim.y / c.heads;
     // the blocks that see most first
-    const int split = blockIdx.x, head = blockIdx.y % c.heads, block = blocks - 1 - blockIdx.y / c.heads, r = blockIdx.z;
+    const int split = split_of_group(), head = blockIdx.y % c.heads, block = blocks - 1 - blockIdx.y / c.heads, r = blockIdx.z;
     Part w;
     if (!part_of(a, r, block, split, w)) return;
     const bool halves = min(w.pairs - w.pair0, a.block_pairs) <= 8 * NT * WAVES;
@@ -1594,6 +1600,9 @@ int cache_args(orloj_worker* w, const orloj_cache* c, const orloj_batch* b, Cach
     if (b->max_length > 1 << 30) return orloj_ctx_fail(x, ORLOJ_E_UNSUPPORTED, "max_length %d > 2^30", b->max_length);
     if (b->n_requests == 0 && b->n_rows > 0)
         return orloj_ctx_fail(x, ORLOJ_E_INVALID, "%lld rows of no requests", (long long)b->n_rows);
+    if (b->n_rows > (int64_t)b->n_requests * b->max_rows)
+        return orloj_ctx_fail(x, ORLOJ_E_INVALID, "%lld rows of %d requests with at most %d each", (long long)b->n_rows,
+                              b->n_requests, b->max_rows);
     if (b->n_rows > 0) {
         if (!c->d_k || !c->d_v || !c->d_k_scale || !c->d_v_scale || !b->d_row_off || !b->d_length || !b->d_pages)
             return orloj_ctx_fail(x, ORLOJ_E_INVALID, "NULL buffer of the cache or the batch");
@@ -1657,14 +1666,17 @@ int cache_copy(orloj_worker* w, const orloj_cache* cache, const orloj_batch* bat
 // few of them, and the join of the splits.
 template <int DP>
 int attend_blocks(orloj_worker* w, AttendArgs& a, const char* what, void (*kernel)(AttendArgs), int threads, int block_pairs,
-                  int per_unit) {
+                  int few, int many) {
     const int64_t pairs = (int64_t)a.c.max_rows * a.group, blocks = (pairs + block_pairs - 1) / block_pairs;
     a.block_pairs = block_pairs;
     const int64_t groups = (int64_t)a.c.requests * a.c.heads * blocks;
-    // per_unit workgroups a unit where there are fewer, from at least 256 tokens each:
-    // the two that a unit holds at once.  More even out requests of different lengths but
-    // begin, end and join more often: 3, 4, 6 or 8 a unit against 2, with 4 to 128
-    // requests of 64 to 8192 tokens, took 0.9 to 1.4 times as long
+    // Where workgroups are fewer than that, few a unit (the two it holds at once, or the two
+    // rounds of them that trees like better), from at least 256 tokens each; where there is
+    // one for every unit, `many`, which evens out requests of different lengths.  us with 2 /
+    // 8 a unit over 8 heads: 4 requests of 64 to 16384 tokens 24 / 29, 16 to 8192 42 / 44, 64
+    // to 8192 140 / 122 (8000 to 8192: 190 / 203); trees of 16 requests with 4 / 8 76 / 86, of 64
+    // 295 / 200
+    const int per_unit = groups < w->ctx->n_cu ? few : many;
     const int64_t want = (per_unit * (int64_t)w->ctx->n_cu + groups - 1) / groups;
     const int64_t most = std::max<int64_t>(1, (a.c.max_length + 255) / 256);
     const int64_t parts = std::min(want, most);
@@ -1692,14 +1704,14 @@ int attend_dim(orloj_worker* w, AttendArgs& a) {
     // up to 32 pairs a wave each takes all of them (64 requests of up to 8192 tokens, 32
     // pairs: 151 us, 224 us in attend_rows_kernel); up to 128 four waves leave two workgroups
     // a unit (16 requests of 96 pairs: 97 us, 117 us with eight; but 64 of 80: 332 and 297)
-    if (pairs <= 16) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, FINE, DP, 1>, kThreads, 16, 2);
+    if (pairs <= 16) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, FINE, DP, 1>, kThreads, 16, 2, 8);
     // beyond 128 dimensions the registers hold the sums of 16 pairs a wave
     if constexpr (DP <= 128) {
-        if (pairs <= 32) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, FINE, DP, 2>, kThreads, 32, 2);
-        if (pairs > 128) return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, FINE, DP, 2, 8>, 512, 256, 2);
-        return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, FINE, DP, 2, 4>, kThreads, 128, 2);
+        if (pairs <= 32) return attend_blocks<DP>(w, a, "attend_kernel", attend_kernel<FMT, FINE, DP, 2>, kThreads, 32, 2, 8);
+        if (pairs > 128) return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, FINE, DP, 2, 8>, 512, 256, 2, 2);
+        return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, FINE, DP, 2, 4>, kThreads, 128, 4, 8);
     } else {
-        return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, FINE, DP, 1, 8>, 512, 128, 2);
+        return attend_blocks<DP>(w, a, "attend_rows_kernel", attend_rows_kernel<FMT, FINE, DP, 1, 8>, 512, 128, 2, 2);
     }
 }
 
@@ -1827,7 +1839,7 @@ int orloj_worker_attend(orloj_worker* w, const orloj_cache* cache, const orloj_b
     if (n_q_heads > 65535 || a.c.requests > 65535)
         return orloj_ctx_fail(w->ctx, ORLOJ_E_UNSUPPORTED, "more than 65535 heads or requests");
     if (int rc = enter(w)) return rc;
-    if (!a.c.rows || !a.c.max_rows) return ORLOJ_OK;
+    if (!a.c.rows) return ORLOJ_OK;
     a.tree = d_tree;
     a.lse = d_lse;
     a.scale = scale;

@@ -11,7 +11,9 @@ step that depend on that:
 
 Argument marshalling only, as in orloj.py: the work is done in the HIP kernels of
 liborloj.so, there is no fallback.  Calls enqueue on the stream of the worker's
-context and return tensors that are ready in that stream's order.
+context and return tensors that are ready in that stream's order; where that is not
+torch's current stream, make it so around the calls (torch.cuda.stream), since the
+tensors they return are torch's to reuse in the order of its own.
 """
 from __future__ import annotations
 

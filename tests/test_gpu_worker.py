@@ -667,6 +667,7 @@ def test_refusals(worker):
     refused(O.ORLOJ_E_UNSUPPORTED, lambda: c.attend(batch_of(65, 65), z(65, 2, 64), tree=z(65, dtype=torch.int64)))
     refused(O.ORLOJ_E_INVALID, lambda: c.attend(batch_of(n_rows=2, max_rows=-1, max_length=4), z(2, 2, 64)))
     refused(O.ORLOJ_E_UNSUPPORTED, lambda: c.read(batch_of(n_rows=2, max_rows=2, max_length=(1 << 30) + 1)))
+    refused(O.ORLOJ_E_INVALID, lambda: c.attend(batch_of(n_rows=2, max_rows=1, max_length=4), z(2, 2, 64)))
     for bad in (lambda: W.Cache(worker, c.k, c.v, c.k_scale, c.v_scale, 65),
                 lambda: W.Cache(worker, c.k, c.v, c.k_scale[:2], c.v_scale, 64),
                 lambda: c.write(b, z(2, 2, 63), z(2, 2, 64)), lambda: c.write(b, z(3, 2, 64), z(2, 2, 64)),
