@@ -8,7 +8,6 @@
 //   attend_kernel, attend_rows_kernel,   attention of the rows over the pages: few (row,
 //   attend_join_kernel                   head) pairs a request, many, and their splits
 
-#include <hip/hip_fp8.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
